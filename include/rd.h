@@ -326,6 +326,94 @@ int rd_set_attention_path(rd_session* s, int32_t path);
  * to the order of the float32 sums; for measurement (A/B) and tests. */
 int rd_set_fused_swiglu(rd_session* s, int32_t on);
 
+/* ---- Paged K/V cache -------------------------------------------------------------------------------
+ * For callers that hand cache memory out page by page instead of reserving max_context positions per
+ * sequence: pages of page_size positions lie anywhere in a pool, a table names the pages of a sequence
+ * in order, and one call works on whatever rows (new tokens) a step has: prompts, slices of prompts,
+ * wavefronts, single tokens, mixed.  (The paper has no counterpart; its Appendix, "Larger Batch
+ * Sizes", asks for requests joining and leaving a running batch.)  A paged session
+ * (rd_session_create_paged, below) runs its layers on the same operators.
+ *
+ * A row at position p of its sequence sees the keys j <= p; with window > 0 only those with
+ * j > p - window, and the first `sinks` positions, which stay visible.  n_heads may be a multiple of
+ * n_kv_heads: query head h reads K/V head h / (n_heads / n_kv_heads). */
+typedef struct rd_paged rd_paged; /* opaque: geometry, rotary table, workspace, (owned) pages */
+
+typedef struct {
+    int32_t n_heads, n_kv_heads, head_dim; /* n_heads a multiple of n_kv_heads; head_dim even, <= 128  */
+    int32_t dtype;                         /* RD_F32 | RD_BF16: type of q, k, v, output and pages      */
+    int32_t page_size;                     /* positions of a page: 16, 32, 64, 128 or 256              */
+    int32_t n_pages;                       /* pages of a layer's pool                                  */
+    int32_t n_layers;                      /* layers that share page numbers; each has its own pool    */
+    int32_t max_context;                   /* positions of a sequence (size of the rotary table)       */
+    int32_t max_rows;                      /* rows of a call; 0: 65536                                 */
+    float rope_base;                       /* rotary base; 0: q and k are stored as they are given     */
+} rd_paged_config;
+
+/* The rows of a call.  Rows are listed by groups, a group being the rows of one sequence; their order
+ * inside a group is free.  Everything the device pointers name is read when the kernels run. */
+typedef struct {
+    int32_t n_rows;              /* rows of the call, at most max_rows                                 */
+    int32_t n_groups;            /* 1 .. 4096                                                          */
+    const int32_t* group_start;  /* device [n_groups + 1], ascending: group i holds rows group_start[i]
+                                    .. group_start[i+1]-1; rows outside every group are left alone.
+                                    NULL: group i holds rows i * max_group_rows ..                     */
+    int32_t max_group_rows;      /* most rows of a group (0: not known).  With group_start it only
+                                    chooses kernels; results do not depend on its being right          */
+    const int32_t* row_pos;      /* device [n_rows]: position of the row in its sequence; negative: no
+                                    row (its outputs are left as they are, nothing is written for it)  */
+    const int32_t* table;        /* device [n_groups, table_stride]: page of positions
+                                    page_size * i .. of the group's sequence; entries no row needs may
+                                    hold anything                                                      */
+    int32_t table_stride;
+} rd_paged_rows;
+
+/* rd_paged_create -- a cache on the current device.
+ *   k_pages, v_pages  device memory [n_layers][n_pages][n_kv_heads][page_size][head_dim] each, 16-byte
+ *                 aligned, that the caller keeps alive as long as the cache (several caches may share it);
+ *                 both NULL: the library allocates it, zero-filled (rd_paged_pages tells where).
+ * One workspace belongs to the cache: its calls must run one after another (one stream, or streams that the
+ * caller orders; likewise replays of CUDA graphs that captured them).  Work that is to overlap takes a
+ * cache of its own over the same pages.  Calls allocate nothing, synchronise nothing and may be captured.
+ * Errors: INVALID_ARG, OOM, CUDA, CAPACITY (more than 2^31 - 512 pool rows
+ * n_layers * n_pages * n_kv_heads * page_size). */
+int rd_paged_create(const rd_paged_config* cfg, void* k_pages, void* v_pages, rd_paged** out);
+/* Waits for the device, then frees what the library allocated. */
+void rd_paged_destroy(rd_paged* c);
+int rd_paged_pages(const rd_paged* c, void** k_pages, void** v_pages);
+
+/* rd_paged_append -- the new rows' q and k turned by the rotary embedding of their positions (adjacent
+ * pairs, angle pos * base^(-2i/d); none with rope_base 0), q to q_out, k and v into the row's place in its
+ * page of `layer`.  Device pointers; strides in elements between rows (heads and features contiguous).
+ * q_out may be q (same stride); apart from that no two of the arrays may overlap.  Rows of one call must not name
+ * the same place twice.
+ * Alignment: with head_dim a multiple of 16 bytes, arrays and row strides multiples of 16 bytes;
+ * with other head_dim of four elements (head_dim a multiple of 4) or two.
+ * Errors: INVALID_ARG, CAPACITY (n_rows), STATE (another device is current), CUDA.  What only the device can
+ * see (a position beyond the table or max_context, a table entry that is no page) skips the row and is
+ * reported by rd_paged_sync. */
+int rd_paged_append(rd_paged* c, const rd_paged_rows* rows, int32_t layer, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                    const void* v, int64_t ldv, void* q_out, int64_t ldqo, void* cuda_stream);
+
+/* rd_paged_attend -- out[r, h] = sum_j p_j V[j], p = softmax over the keys j row r sees of scale * q[r, h] . K[j].
+ *   q, out        device, rows of n_heads * head_dim, strides in elements; alignment as above; no overlap.
+ *   lse           device float32 [n_rows, n_heads] receiving ln sum_j exp(scale * q . K[j]), or NULL.
+ *   window        0: every key j <= p; else the newest `window` of them (>= 1) and the first `sinks`.
+ *   scale         > 0, or 0 for 1 / sqrt(head_dim).
+ * The K and V of every key a row sees must have been appended.  Scores, sums and outputs are accumulated in
+ * float32; with RD_BF16 the probabilities are rounded to bf16 for the product with V.  Results do not depend
+ * on timing: the same call gives the same bits.  A key a row does not see has no influence on it, whatever its
+ * page holds.
+ * Errors: as rd_paged_append. */
+int rd_paged_attend(rd_paged* c, const rd_paged_rows* rows, int32_t layer, const void* q, int64_t ldq, void* out, int64_t ldo,
+                    float* lse, int32_t window, int32_t sinks, float scale, void* cuda_stream);
+
+/* rd_paged_sync -- waits for the stream and reports what kernels of this cache saw since the last call:
+ * INVALID_ARG (a row beyond the table or max_context, a needed table entry that is no page, a group_start that
+ * does not ascend: those rows' results are undefined) or TIMEOUT (a bounded wait ran out; reported from then on:
+ * destroy the cache). */
+int rd_paged_sync(rd_paged* c, void* cuda_stream);
+
 const char* rd_strerror(int code);
 /* Text of the last CUDA error this library saw on the calling thread's most recent failing call
  * (static storage, never NULL). */

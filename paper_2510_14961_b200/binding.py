@@ -20,7 +20,8 @@ EXPORTS = ["rd_load", "rd_free", "rd_session_create", "rd_session_destroy", "rd_
            "rd_last_cuda_error", "rd_profile_enable", "rd_profile_read", "rd_debug_read_kv_noalloc", "rd_set_launch_chaining",
            "rd_debug_expire_next_wait", "rd_set_fused_swiglu", "rd_set_attention_path", "rd_poll_begin", "rd_poll_end",
            "rd_debug_gemm_sequence", "rd_prefill_sliced", "rd_prefill_advance", "rd_prefill_pending",
-           "rd_set_prefill_units"]
+           "rd_set_prefill_units", "rd_paged_create", "rd_paged_destroy", "rd_paged_pages", "rd_paged_append", "rd_paged_attend",
+           "rd_paged_sync"]
 
 
 class RdConfig(C.Structure):
@@ -34,6 +35,16 @@ class RdSessionConfig(C.Structure):
                                          "max_new_tokens", "keep_logits")] + \
                [("temperature", C.c_float), ("seed", C.c_uint64), ("eta", C.c_float), ("beta", C.c_float),
                 ("top_p", C.c_float), ("latent_slots", C.c_int32)]
+
+
+class RdPagedConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "dtype", "page_size", "n_pages", "n_layers",
+                                         "max_context", "max_rows")] + [("rope_base", C.c_float)]
+
+
+class RdPagedRows(C.Structure):
+    _fields_ = [("n_rows", C.c_int32), ("n_groups", C.c_int32), ("group_start", C.c_void_p), ("max_group_rows", C.c_int32),
+                ("row_pos", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int32)]
 
 
 class RdStats(C.Structure):
@@ -97,6 +108,14 @@ def lib():
         L.rd_poll_end.argtypes = [vp, i32, i32, C.POINTER(i32), C.POINTER(i32)]
         L.rd_profile_enable.argtypes = [vp, i32]
         L.rd_profile_read.argtypes = [vp, C.POINTER(RdProfile)]
+        i64 = C.c_int64
+        L.rd_paged_create.argtypes = [C.POINTER(RdPagedConfig), vp, vp, C.POINTER(vp)]
+        L.rd_paged_destroy.argtypes = [vp]
+        L.rd_paged_destroy.restype = None
+        L.rd_paged_pages.argtypes = [vp, C.POINTER(vp), C.POINTER(vp)]
+        L.rd_paged_append.argtypes = [vp, C.POINTER(RdPagedRows), i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        L.rd_paged_attend.argtypes = [vp, C.POINTER(RdPagedRows), i32, vp, i64, vp, i64, vp, i32, i32, f32, vp]
+        L.rd_paged_sync.argtypes = [vp, vp]
         L.rd_strerror.argtypes = [C.c_int]
         L.rd_strerror.restype = C.c_char_p
         L.rd_last_cuda_error.restype = C.c_char_p
@@ -296,3 +315,102 @@ class Session:
         pr = RdProfile()
         _check(lib().rd_profile_read(self.handle, C.byref(pr)), "rd_profile_read")
         return {k: getattr(pr, k) for k, _ in RdProfile._fields_}
+
+
+class PagedRows:
+    """The rows of a paged call (rd_paged_rows): device tensors of int32.
+
+    row_pos [n_rows]: position of every row in its sequence, negative: no row.  table [n_groups, pages]: the
+    sequences' pages in order.  group_start [n_groups + 1]: group i holds rows group_start[i] ..; None: every
+    group holds `max_group_rows` rows.  The tensors are read when the kernels run: keep them alive (this object
+    does) and change them only behind the calls that use them."""
+
+    def __init__(self, row_pos, table, group_start=None, max_group_rows=0):
+        for name, t, dims in (("row_pos", row_pos, 1), ("table", table, 2), ("group_start", group_start, 1)):
+            if t is None and name == "group_start":
+                continue
+            if t.dim() != dims or t.element_size() != 4 or t.is_floating_point() or not t.is_cuda:
+                raise ValueError(f"{name}: a device tensor of int32 with {dims} dimension(s)")
+            if t.numel() and t.stride(-1) != 1:
+                raise ValueError(f"{name}: not contiguous")
+        n_groups, pages = table.shape
+        if group_start is not None and group_start.numel() != n_groups + 1:
+            raise ValueError("group_start: one entry per group and one more")
+        self.row_pos, self.table, self.group_start = row_pos, table, group_start
+        self.c = RdPagedRows(row_pos.numel(), n_groups, _ptr(group_start), max_group_rows, _ptr(row_pos), _ptr(table),
+                             table.stride(0) if n_groups > 1 else pages)
+
+
+class PagedCache:
+    """rd_paged_create and the calls on a paged K/V cache.
+
+    k_pages, v_pages: device tensors [n_layers, n_pages, n_kv_heads, page_size, head_dim] of the cache's type, or
+    None: the library allocates them.  stream: the CUDA stream of calls that name none (None: the legacy default
+    stream).  Calls of one cache run one after another; see include/rd.h."""
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, page_size, n_pages, n_layers=1, max_context=4096, dtype=RD_BF16,
+                 rope_base=10000.0, max_rows=0, k_pages=None, v_pages=None, stream=None):
+        self.cfg = RdPagedConfig(n_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, n_layers, max_context, max_rows, rope_base)
+        self.handle = C.c_void_p()
+        self.stream = stream
+        for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+            if t is None:
+                continue
+            self._typed(name, t)
+            if t.numel() != n_layers * n_pages * n_kv_heads * page_size * head_dim or not t.is_contiguous():
+                raise ValueError(f"{name}: contiguous [n_layers, n_pages, n_kv_heads, page_size, head_dim]")
+        self._keep = (k_pages, v_pages)
+        _check(lib().rd_paged_create(C.byref(self.cfg), _ptr(k_pages), _ptr(v_pages), C.byref(self.handle)), "rd_paged_create")
+
+    def _typed(self, name, t):
+        if not t.is_cuda or not str(t.dtype).endswith("bfloat16" if self.cfg.dtype == RD_BF16 else "float32"):
+            raise ValueError(f"{name}: a device tensor of the cache's type")
+
+    def _rows(self, name, t, n_rows, heads):
+        """Address and row stride of [n_rows, heads, head_dim] (or [n_rows, heads * head_dim])."""
+        self._typed(name, t)
+        d = self.cfg.head_dim
+        if tuple(t.shape) not in ((n_rows, heads, d), (n_rows, heads * d)):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, wanted ({n_rows}, {heads}, {d})")
+        inner = t.stride()[1:]
+        if t.numel() and (inner[-1] != 1 or (t.dim() == 3 and heads > 1 and inner[0] != d)):
+            raise ValueError(f"{name}: heads and features must be contiguous")
+        return t.data_ptr(), (t.stride(0) if n_rows > 1 else heads * d)
+
+    def _stream(self, stream):
+        return C.c_void_p((self.stream if stream is None else stream) or 0)
+
+    def append(self, rows, q, k, v, q_out, layer=0, stream=None):
+        n, c = rows.c.n_rows, self.cfg
+        args = []
+        for name, t, h in (("q", q, c.n_heads), ("k", k, c.n_kv_heads), ("v", v, c.n_kv_heads), ("q_out", q_out, c.n_heads)):
+            args += self._rows(name, t, n, h)
+        _check(lib().rd_paged_append(self.handle, C.byref(rows.c), layer, *args, self._stream(stream)), "rd_paged_append")
+
+    def attend(self, rows, q, out, lse=None, layer=0, window=0, sinks=0, scale=0.0, stream=None):
+        n, c = rows.c.n_rows, self.cfg
+        qa, oa = self._rows("q", q, n, c.n_heads), self._rows("out", out, n, c.n_heads)
+        if lse is not None and (tuple(lse.shape) != (n, c.n_heads) or lse.element_size() != 4 or not lse.is_contiguous() or not lse.is_cuda):
+            raise ValueError(f"lse: contiguous float32 ({n}, {c.n_heads})")
+        _check(lib().rd_paged_attend(self.handle, C.byref(rows.c), layer, *qa, *oa, _ptr(lse), window, sinks, scale, self._stream(stream)),
+               "rd_paged_attend")
+
+    def pages(self):
+        """Device addresses of the K and the V pages."""
+        k, v = C.c_void_p(), C.c_void_p()
+        _check(lib().rd_paged_pages(self.handle, C.byref(k), C.byref(v)), "rd_paged_pages")
+        return k.value, v.value
+
+    def sync(self, stream=None):
+        _check(lib().rd_paged_sync(self.handle, self._stream(stream)), "rd_paged_sync")
+
+    def close(self):
+        if self.handle:
+            lib().rd_paged_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

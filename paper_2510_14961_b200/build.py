@@ -7,8 +7,9 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librd_b200.so")
-SOURCES = ["rd_lib.cu"]
-HEADERS = ["rd_common.cuh", "rd_partial.cuh", "rd_kernels.cuh", "rd_gemm_tc.cuh", "rd_attn.cuh", "rd_attn_tc.cuh", os.path.join("..", "..", "include", "rd.h")]
+SOURCES = ["rd_lib.cu", "rd_paged.cu"]
+HEADERS = ["rd_common.cuh", "rd_partial.cuh", "rd_kernels.cuh", "rd_gemm_tc.cuh", "rd_attn.cuh", "rd_attn_tc.cuh", "rd_paged.cuh",
+           "rd_paged_host.h", "rd_paged_mma.cuh", "rd_paged_simt.cuh", "rd_paged_tc.cuh", os.path.join("..", "..", "include", "rd.h")]
 
 
 def _stale() -> bool:
@@ -23,7 +24,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-o", LIB] + SOURCES
+           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-t", "0", "-o", LIB] + SOURCES
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")

@@ -18,6 +18,7 @@
 #include "rd_attn_tc.cuh"
 #include "rd_gemm_tc.cuh"
 #include "rd_kernels.cuh"
+#include "rd_paged_host.h"
 
 using namespace rd;
 
@@ -26,11 +27,12 @@ using namespace rd;
 // ---------------------------------------------------------------------------------------------
 static thread_local char g_cuda_err[320] = "no CUDA error recorded";
 
-static int cuda_fail(cudaError_t e, const char* what, int line) {
-    snprintf(g_cuda_err, sizeof g_cuda_err, "%s (%s) at rd_lib.cu:%d: %s", cudaGetErrorName(e), what, line,
+int rd::cuda_fail_at(cudaError_t e, const char* what, const char* file, int line) {
+    snprintf(g_cuda_err, sizeof g_cuda_err, "%s (%s) at %s:%d: %s", cudaGetErrorName(e), what, file, line,
              cudaGetErrorString(e));
     return e == cudaErrorMemoryAllocation ? RD_E_OOM : RD_E_CUDA;
 }
+static int cuda_fail(cudaError_t e, const char* what, int line) { return cuda_fail_at(e, what, "rd_lib.cu", line); }
 #define CU(expr)                                                        \
     do {                                                                \
         cudaError_t e_ = (expr);                                        \

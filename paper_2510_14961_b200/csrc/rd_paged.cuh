@@ -1,0 +1,550 @@
+// Paged K/V cache: what its kernels share (arguments, row spans, the division of the work, the joining of
+// partial results), and the kernel that writes new rows into the pages.
+//
+// Pages: [layer][page][kv head][page_size][head_dim] for K and for V; a sequence's positions
+// page_size * i .. page_size * (i + 1) - 1 lie on page table[group][i].  A call names rows (one new token
+// each) by groups: the rows of one sequence, every row with its position.  A row at position p sees the keys
+// j <= p of its sequence, with a window w > 0 only those with j > p - w or j < sinks.
+//
+// The g = n_heads / n_kv_heads query heads that share a K/V head are extra rows of the same product:
+// "packed" row i of a group is head i % g of its row i / g.  A row tile is M consecutive packed rows, and
+// its keys are those at least one of its rows sees, in tiles of KT keys: first the tiles of the sinks, then
+// those from the oldest key inside a window to the newest position.
+//
+// Division of the work.  Key tiles of all (row tile, kv head) items are numbered in one sequence and cut
+// into one equal contiguous share per block, whatever the batch looks like: one sequence of 131,072
+// positions is split over all SMs, 64 ragged ones are packed onto them.  An item that lies in one share is
+// finished there; the shares of an item that is cut leave (maximum, sum, unnormalised output) in a workspace,
+// and the block that arrives last joins them in key order, so results do not depend on which block that is.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "rd_common.cuh"
+#include "rd_partial.cuh"
+
+namespace rd {
+
+struct PgBatch {
+    int n_rows, n_groups;
+    int uniform;                 // rows per group when group_start is null
+    const int* group_start;      // [n_groups + 1], or null
+    const int* row_pos;          // [n_rows]; negative: the row belongs to no sequence
+    const int* table;            // [n_groups][table_stride]
+    int table_stride;
+};
+struct PgGeom {
+    int n_heads, n_kv, g, D;
+    int page_shift, n_pages, layer;
+    int max_pos;                 // positions the rotary table covers
+};
+// Device status word: bits a kernel raises, turned into an error code when the cache is synchronised.
+constexpr int PG_ST_TIMEOUT = 1, PG_ST_BAD_ROW = 2, PG_ST_BAD_PAGE = 4;
+
+struct PgRecord {                // one row tile
+    int grp, a, n, rt;           // group, its first row, its rows, number of the tile in the group
+    int pmin, pmax, nt, pad;     // smallest and largest position of its rows, key tiles
+};
+struct PgWork {                  // one launch's share of the workspace
+    PgRecord* rec;               // external plan: records, with their number in *n_rec
+    int* n_rec;
+    int* counter;                // [blocks] shares of the cut item that starts in a block which have arrived; 0 between launches
+    float* part;                 // [2 * blocks][M][D + 2]
+    int* status;
+};
+struct PgAttend {
+    PgBatch b;
+    PgGeom ge;
+    PgWork w;
+    const void* q; void* out; float* lse;
+    long long ldq, ldo;          // elements between rows
+    const void *k, *v;           // pages (the kernels without tensor maps)
+    int window, sinks;
+    float scale_log2;            // scale * log2(e)
+    int packed_lo, packed_hi;    // groups with packed_lo < packed rows <= packed_hi are this launch's
+    int inline_plan;             // every block makes the plan itself (few row tiles)
+    int min_share;               // key tiles a share has at least
+    int rec_cap;                 // row tiles the plan's array holds (more only come from a group_start that is not ascending)
+};
+
+__device__ __forceinline__ void pg_group_rows(const PgBatch& b, int i, int* a, int* n) {
+    int lo, hi;
+    if (b.group_start) { lo = b.group_start[i]; hi = b.group_start[i + 1]; }
+    else { const long long f = (long long)i * b.uniform; lo = (int)min(f, (long long)b.n_rows); hi = (int)min(f + b.uniform, (long long)b.n_rows); }
+    lo = max(0, min(lo, b.n_rows));
+    hi = max(lo, min(hi, b.n_rows));
+    *a = lo;
+    *n = hi - lo;
+}
+// Positions a call may name: those the table row and the rotary table cover.
+__device__ __forceinline__ int pg_pos_limit(const PgBatch& b, const PgGeom& ge) {
+    const long long t = (long long)b.table_stride << ge.page_shift;
+    return (int)min(t, (long long)ge.max_pos);
+}
+// Row of the [layers * pages * kv heads * page_size, D] view of the pages that holds position `key` of group
+// `grp`, or -1 when its table entry is no page.
+__device__ __forceinline__ long long pg_row_of(const PgBatch& b, const PgGeom& ge, int grp, int kvh, int key) {
+    const int pi = key >> ge.page_shift;
+    if (pi >= b.table_stride) return -1;
+    const int pg = b.table[(size_t)grp * b.table_stride + pi];
+    if (pg < 0 || pg >= ge.n_pages) return -1;
+    return ((((long long)ge.layer * ge.n_pages + pg) * ge.n_kv + kvh) << ge.page_shift) + (key & ((1 << ge.page_shift) - 1));
+}
+
+// Key tiles of a row tile.  lo: first tile inside the window; ns: tiles of the sinks in front of it.
+struct PgSpan { int nt, ns, lo; };
+template <int KT>
+__device__ __forceinline__ PgSpan pg_span(int pmin, int pmax, int window, int sinks) {
+    PgSpan s = {0, 0, 0};
+    if (pmax < 0) return s;
+    const int lo_key = window > 0 ? max(0, pmin - window + 1) : 0;
+    s.lo = lo_key / KT;
+    if (window > 0) s.ns = min((min(sinks, pmax + 1) + KT - 1) / KT, s.lo);
+    s.nt = s.ns + pmax / KT + 1 - s.lo;
+    return s;
+}
+__device__ __forceinline__ int pg_tile_key(const PgSpan& s, int i, int kt) { return (i < s.ns ? i : i - s.ns + s.lo) * kt; }
+// Whether row position p (>= 0) sees key j.
+__device__ __forceinline__ bool pg_sees(int p, int j, int window, int sinks) {
+    return j <= p && (window <= 0 || p - j < window || j < sinks);
+}
+// Whether some row of a row tile does not see some key of the tile that starts at key0.
+template <int KT> __device__ __forceinline__ bool pg_partial(int key0, int pmin, int pmax, int window, int sinks) {
+    return key0 + KT - 1 > pmin || (window > 0 && pmax - key0 >= window && key0 + KT > sinks);
+}
+
+// ---- the plan -----------------------------------------------------------------------------------------------
+constexpr int PG_MAX_GROUPS = 4096;       // groups of a call
+constexpr int PG_INLINE_REC = 256;        // row tiles a block plans by itself
+
+// Lanes that look at the rows of one row tile together.
+__host__ __device__ __forceinline__ int pg_lanes(int M, int g) {
+    const int rows = (M + g - 1) / g + 1;
+    int l = 1;
+    while (l < 32 && l * 4 < rows) l *= 2;
+    return l;
+}
+// Positions of a row tile by `lanes` neighbouring lanes (all 32 lanes of the warp call this).
+__device__ __forceinline__ void pg_tile_positions(const PgBatch& b, const PgGeom& ge, int M, int a, int n, int rt, bool valid, int lanes,
+                                                  int lane_in, int limit, int* pmin, int* pmax, bool* bad) {
+    int lo = 0x7fffffff, hi = -1;
+    if (valid) {
+        const int r0 = (int)((long long)rt * M / ge.g);
+        const int r1 = (int)min((long long)n, ((long long)(rt + 1) * M + ge.g - 1) / ge.g);
+#pragma unroll 8
+        for (int r = r0 + lane_in; r < r1; r += lanes) {
+            const int p = b.row_pos[a + r];
+            if (p >= limit) *bad = true;
+            else if (p >= 0) { lo = min(lo, p); hi = max(hi, p); }
+        }
+    }
+    for (int s = 1; s < lanes; s *= 2) {
+        lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, s));
+        hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, s));
+    }
+    *pmin = hi < 0 ? -1 : lo;
+    *pmax = hi;
+}
+// Exclusive prefix sum over the block's threads (NT threads, NT a multiple of 32); *total: the sum.
+template <int NT, typename V> __device__ __forceinline__ V pg_block_scan(V v, V* warp_sums, V* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    V inc = v;
+#pragma unroll
+    for (int s = 1; s < 32; s *= 2) {
+        const V o = __shfl_up_sync(0xffffffffu, inc, s);
+        if (lane >= s) inc += o;
+    }
+    __syncthreads();
+    if (lane == 31) warp_sums[warp] = inc;
+    __syncthreads();
+    V base = 0, tot = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; w++) {
+        const V x = warp_sums[w];
+        if (w < warp) base += x;
+        tot += x;
+    }
+    *total = tot;
+    return base + inc - v;
+}
+
+// Row tiles of all groups: `first` (shared memory, n_groups entries) receives the number of the first
+// row tile of every group; returns how many there are.
+template <int NT>
+__device__ int pg_count_tiles(const PgAttend& p, int M, int* first, int* warp_sums) {
+    const int ng = p.b.n_groups;
+    int base = 0;
+    for (int c0 = 0; c0 < ng; c0 += NT) {
+        const int i = c0 + (int)threadIdx.x;
+        int t = 0;
+        if (i < ng) {
+            int a, n;
+            pg_group_rows(p.b, i, &a, &n);
+            const long long packed = (long long)n * p.ge.g;
+            if (packed > p.packed_lo && packed <= p.packed_hi) t = (int)((packed + M - 1) / M);
+        }
+        int tot;
+        const int at = pg_block_scan<NT, int>(t, warp_sums, &tot);
+        if (i < ng) first[i] = base + at;
+        base += tot;
+    }
+    if (base > p.rec_cap) {
+        if (threadIdx.x == 0) atomicOr(p.w.status, PG_ST_BAD_ROW);
+        base = p.rec_cap;
+    }
+    __syncthreads();
+    return base;
+}
+// Records r0, r0 + step, ... of the n_rec row tiles (each by `lanes` lanes) into dst.
+template <int NT, int KT>
+__device__ void pg_make_records(const PgAttend& p, int M, const int* first, int n_rec, PgRecord* dst, int part, int n_parts) {
+    const int lanes = pg_lanes(M, p.ge.g), per_block = NT / lanes;
+    const int lane_in = (int)threadIdx.x % lanes, slot = (int)threadIdx.x / lanes;
+    const int limit = pg_pos_limit(p.b, p.ge);
+    bool bad = false;
+    for (int r0 = part * per_block; r0 < n_rec; r0 += n_parts * per_block) {
+        const int r = r0 + slot;
+        const bool valid = r < n_rec;
+        PgRecord rec = {};
+        if (valid) {
+            int lo = 0, hi = p.b.n_groups - 1;             // last group whose first tile is <= r
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (first[mid] <= r) lo = mid; else hi = mid - 1;
+            }
+            rec.grp = lo;
+            pg_group_rows(p.b, lo, &rec.a, &rec.n);
+            rec.rt = r - first[lo];
+        }
+        pg_tile_positions(p.b, p.ge, M, rec.a, rec.n, rec.rt, valid, lanes, lane_in, limit, &rec.pmin, &rec.pmax, &bad);
+        rec.nt = pg_span<KT>(rec.pmin, rec.pmax, p.window, p.sinks).nt;
+        if (valid && lane_in == 0) dst[r] = rec;
+    }
+    if (bad) atomicOr(p.w.status, PG_ST_BAD_ROW);
+}
+
+// The plan as a kernel of its own, for calls with many row tiles.  Dynamic shared memory: n_groups ints.
+constexpr int PG_PLAN_THREADS = 256;
+template <int KT>
+__global__ void __launch_bounds__(PG_PLAN_THREADS) pg_plan_kernel(const __grid_constant__ PgAttend p, int M) {
+    extern __shared__ int first[];
+    __shared__ int warp_sums[PG_PLAN_THREADS / 32];
+    pdl_enter();
+    const int n_rec = pg_count_tiles<PG_PLAN_THREADS>(p, M, first, warp_sums);
+    pg_make_records<PG_PLAN_THREADS, KT>(p, M, first, n_rec, p.w.rec, blockIdx.x, gridDim.x);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.w.n_rec = n_rec;
+}
+
+// A block's share: units [u0, u1) of the numbered key tiles, and where u0 lies.
+struct PgShare {
+    long long u0, u1, per;
+    int rec, head, tile, n_rec;
+};
+template <int CAP> struct PgPlanSmem {
+    PgRecord rec[CAP];           // CAP = PG_INLINE_REC, or 1 for a kernel whose plan is always made before it
+    int first[CAP];
+    long long warp_sums[32];
+    int warp_sums_i[32];
+    PgShare share;
+};
+// All NT threads call this; the plan ends in sm.share, records in sm.rec (inline) or p.w.rec.
+template <int NT, int KT, int CAP>
+__device__ void pg_plan_share(const PgAttend& p, int M, PgPlanSmem<CAP>& sm) {
+    int n_rec;
+    const PgRecord* rec = p.w.rec;
+    if (CAP > 1 && p.inline_plan) {
+        n_rec = pg_count_tiles<NT>(p, M, sm.first, sm.warp_sums_i);
+        pg_make_records<NT, KT>(p, M, sm.first, n_rec, sm.rec, 0, 1);
+        rec = sm.rec;
+        __syncthreads();
+    } else {
+        n_rec = *p.w.n_rec;
+    }
+    const int chunk = (n_rec + NT - 1) / NT, r0 = min(n_rec, (int)threadIdx.x * chunk), r1 = min(n_rec, r0 + chunk);
+    long long mine = 0;
+    for (int r = r0; r < r1; r++) mine += rec[r].nt;
+    mine *= p.ge.n_kv;
+    long long total;
+    const long long before = pg_block_scan<NT, long long>(mine, sm.warp_sums, &total);
+    const long long per = max((total + gridDim.x - 1) / gridDim.x, (long long)p.min_share);
+    const long long u0 = min(total, per * blockIdx.x), u1 = min(total, u0 + per);
+    if (threadIdx.x == 0) { sm.share.u0 = u0; sm.share.u1 = u1; sm.share.per = per; sm.share.n_rec = n_rec; sm.share.rec = n_rec; }
+    __syncthreads();
+    if (u0 < u1 && u0 >= before && u0 < before + mine) {
+        long long u = before;
+        for (int r = r0; r < r1; r++) {
+            const long long len = (long long)rec[r].nt * p.ge.n_kv;
+            if (u0 < u + len) {
+                sm.share.rec = r;
+                sm.share.head = (int)((u0 - u) / rec[r].nt);
+                sm.share.tile = (int)((u0 - u) % rec[r].nt);
+                break;
+            }
+            u += len;
+        }
+    }
+    __syncthreads();
+}
+
+// One piece of an item: key tiles [i0, i1) of (row tile, kv head).
+struct PgPiece {
+    int grp, a, n, rt, head, i0, i1, nt, pmin, pmax;
+    int c_first, c_last;         // blocks whose shares hold the item; equal: the piece is the whole item
+};
+// Walks a share piece by piece; every caller that walks (several warps may) sees the same pieces.
+struct PgWalk {
+    long long u, u1, per;
+    int rec, head, tile, n_rec;
+    const PgRecord* recs;
+    template <int CAP> __device__ __forceinline__ void start(const PgAttend& p, const PgPlanSmem<CAP>& sm) {
+        u = sm.share.u0; u1 = sm.share.u1; per = sm.share.per;
+        rec = sm.share.rec; head = sm.share.head; tile = sm.share.tile; n_rec = sm.share.n_rec;
+        recs = CAP > 1 && p.inline_plan ? sm.rec : p.w.rec;
+    }
+    __device__ __forceinline__ bool next(int n_kv, PgPiece* o) {
+        if (u >= u1 || rec >= n_rec) return false;
+        PgRecord r = recs[rec];
+        while (r.nt == 0) {                       // row tiles without a row of a sequence
+            if (++rec >= n_rec) return false;
+            r = recs[rec];
+        }
+        const int len = (int)min((long long)(r.nt - tile), u1 - u);
+        o->grp = r.grp; o->a = r.a; o->n = r.n; o->rt = r.rt; o->head = head;
+        o->i0 = tile; o->i1 = tile + len; o->nt = r.nt; o->pmin = r.pmin; o->pmax = r.pmax;
+        const long long first = u - tile;
+        o->c_first = (int)(first / per);
+        o->c_last = (int)((first + r.nt - 1) / per);
+        u += len;
+        tile += len;
+        if (tile == r.nt) {
+            tile = 0;
+            if (++head == n_kv) { head = 0; rec++; }
+        }
+        return true;
+    }
+};
+
+// Hands registers from the warps that need few to those that need many.  A block of 384 threads is launched with
+// 168 registers a thread (64,512); 2 x 128 threads at 216 and 128 at 72 make the same.
+template <int N> __device__ __forceinline__ void pg_regs_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void pg_regs_less() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+constexpr int PG_REGS_MORE = 216, PG_REGS_LESS = 72;
+
+// ---- partial results ------------------------------------------------------------------------------------------
+// Slot of block c for the item that starts in block c_first: the item is the last of c_first's share and
+// the first of every later one.
+__device__ __forceinline__ float* pg_slot(const PgWork& w, int c, int c_first, int M, int D) {
+    return w.part + (size_t)(2 * c + (c == c_first ? 1 : 0)) * M * (D + 2);
+}
+// To be called by all `threads` threads of a group (barrier `bar`) that have written their share's slot: true
+// in the block that arrives last, which then sees every slot.
+template <typename Sync>
+__device__ __forceinline__ bool pg_arrive_last(const PgWork& w, const PgPiece& pc, bool leader, int* flag, Sync sync) {
+    __threadfence();
+    sync();
+    if (leader) {
+        const int want = pc.c_last - pc.c_first;
+        const int seen = atomicAdd(&w.counter[pc.c_first], 1);
+        const bool last = seen == want;
+        if (last) atomicExch(&w.counter[pc.c_first], 0);       // for the next launch
+        *flag = last;
+        __threadfence();
+    }
+    sync();
+    const bool last = *flag != 0;
+    if (last) __threadfence();
+    return last;
+}
+__device__ __forceinline__ void pg_store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
+__device__ __forceinline__ void pg_store4(__nv_bfloat16* p, float a, float b, float c, float d) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b), y = __floats2bfloat162_rn(c, d);
+    uint2 u;
+    u.x = *reinterpret_cast<const uint32_t*>(&x); u.y = *reinterpret_cast<const uint32_t*>(&y);
+    *reinterpret_cast<uint2*>(p) = u;
+}
+// Joins the shares of an item and writes its rows.  Slot layout: outputs [M][D] (unnormalised, scaled by
+// 2^m), then (m, l) [M][2].  tid counts the `threads` callers, a thread takes V features (4, or 1 when D is not
+// a multiple of 4).
+template <typename T, int V>
+__device__ __forceinline__ void pg_join(const PgAttend& p, const PgPiece& pc, int M, int D, int tid, int threads) {
+    const int rows = (int)min((long long)M, (long long)pc.n * p.ge.g - (long long)pc.rt * M);
+    const int ns = pc.c_last - pc.c_first + 1, q4 = D / V, limit = pg_pos_limit(p.b, p.ge);
+    for (int it = tid; it < rows * q4; it += threads) {
+        const int r = it / q4, e = (it % q4) * V;
+        const long long pk = (long long)pc.rt * M + r;
+        const int row = pc.a + (int)(pk / p.ge.g), hd = pc.head * p.ge.g + (int)(pk % p.ge.g);
+        const int pos = p.b.row_pos[row];
+        if (pos < 0 || pos >= limit) continue;
+        float mx = -INFINITY;
+#pragma unroll 4
+        for (int s = 0; s < ns; s++) mx = fmaxf(mx, __ldcg(pg_slot(p.w, pc.c_first + s, pc.c_first, M, D) + (size_t)M * D + 2 * r));
+        float acc[V], den = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; i++) acc[i] = 0.f;
+#pragma unroll 4
+        for (int s = 0; s < ns; s++) {
+            const float* sl = pg_slot(p.w, pc.c_first + s, pc.c_first, M, D);
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(sl + (size_t)M * D + 2 * r));
+            const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mx);
+            float v[V];
+            if constexpr (V == 4) {
+                const float4 u = __ldcg(reinterpret_cast<const float4*>(sl + (size_t)r * D + e));
+                v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+            } else {
+                v[0] = __ldcg(sl + (size_t)r * D + e);
+            }
+#pragma unroll
+            for (int i = 0; i < V; i++) acc[i] = fmaf(v[i], w, acc[i]);
+            den = fmaf(ml.y, w, den);
+        }
+        const float inv = 1.0f / den;
+        T* dst = (T*)p.out + (size_t)row * p.ldo + hd * D + e;
+        if constexpr (V == 4) pg_store4(dst, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+        else dst[0] = (T)(acc[0] * inv);
+        if (p.lse && e == 0) p.lse[(size_t)row * p.ge.n_heads + hd] = (mx + log2f(den)) * 0.6931471805599453f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void pg_join_any(const PgAttend& p, const PgPiece& pc, int M, int D, int tid, int threads) {
+    if (D % 4 == 0) pg_join<T, 4>(p, pc, M, D, tid, threads);
+    else pg_join<T, 1>(p, pc, M, D, tid, threads);
+}
+
+// ---- new rows into the pages ------------------------------------------------------------------------------------
+// cos/sin of pos * base^(-2i/d), [max_pos][d/2]: angles in double (far positions keep their fraction), stored as float32.
+static __global__ void __launch_bounds__(256) pg_rope_table_kernel(float2* __restrict__ cs, int max_pos, int half, double log2_base) {
+    const long long n = (long long)max_pos * half;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
+        const int p = (int)(i / half), j = (int)(i % half);
+        double s, c;
+        sincos((double)p * exp2(-log2_base * (double)j / (double)half), &s, &c);
+        cs[i] = make_float2((float)c, (float)s);
+    }
+}
+
+template <typename T> __device__ __forceinline__ float pg_to_f(T x) { return (float)x; }
+template <typename T> __device__ __forceinline__ T pg_from_f(float x);
+template <> __device__ __forceinline__ float pg_from_f<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 pg_from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// VEC features at once, as wide as their bytes allow.
+template <typename T, int VEC> struct alignas(sizeof(T) * VEC > 16 ? 16 : sizeof(T) * VEC) PgVec { T x[VEC]; };
+
+// Sources of the new rows: q of feature m (0 .. n_heads D - 1), k and v of feature m (0 .. n_kv D - 1).
+template <typename T> struct PgArrays {                   // three arrays of the cache's type (rd_paged_append)
+    const T *q, *k, *v;
+    long long ldq, ldk, ldv;
+    template <int VEC> __device__ __forceinline__ void load(int what, int r, int m, float* x) const {
+        const T* s = what == 0 ? q + (size_t)r * ldq : what == 1 ? k + (size_t)r * ldk : v + (size_t)r * ldv;
+        const PgVec<T, VEC> u = *reinterpret_cast<const PgVec<T, VEC>*>(s + m);
+#pragma unroll
+        for (int i = 0; i < VEC; i++) x[i] = pg_to_f(u.x[i]);
+    }
+};
+struct PgSums {                                           // sums of a QKV GEMM, [rows][q | k | v] (a session's layer)
+    RowSource src;
+    int nq, nk;                                           // features of q, of k
+    template <int VEC> __device__ __forceinline__ void load(int what, int r, int m, float* x) const {
+        const int at = m + (what == 0 ? 0 : what == 1 ? nq : nq + nk);
+        if constexpr (VEC % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < VEC; i += 4) {
+                const float4 u = row_source_load4(src, r, at + i);
+                x[i] = u.x; x[i + 1] = u.y; x[i + 2] = u.z; x[i + 3] = u.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; i++) x[i] = row_source_load(src, r, at + i);
+        }
+    }
+};
+
+struct PgAppend {
+    PgBatch b;
+    PgGeom ge;
+    int* status;
+    const float2* cs;            // rotary table, or null: q and k are stored as they come
+    void* q_out; long long ldqo;
+    void *k, *v;                 // pages
+};
+
+// Rotary embedding (adjacent pairs) of q and k at the row's position; q to q_out, k and v to the row's place
+// in its page.  Bound by memory: every value is read and written once (the angles come from L1 for all heads
+// but the first), VEC features (16 bytes of bf16) per thread and turn, four loads in flight.  Grid (rows, parts of a row).
+constexpr int PG_APPEND_THREADS = 256;
+template <typename T, int VEC, typename Src>
+__global__ void __launch_bounds__(PG_APPEND_THREADS) pg_append_kernel(const __grid_constant__ PgAppend p, const __grid_constant__ Src src) {
+    __shared__ int grp_s;
+    pdl_enter();
+    const int r = blockIdx.x, D = p.ge.D, per_head = D / VEC;
+    const int items = (p.ge.n_heads + 2 * p.ge.n_kv) * per_head, stride = gridDim.y * PG_APPEND_THREADS;
+    const int pos = p.b.row_pos[r];
+    if (pos < 0) return;
+    int grp;
+    if (p.b.group_start) {
+        // the row's group: one look at the group borders by all threads together
+        if (threadIdx.x == 0) grp_s = -1;
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.b.n_groups; i += PG_APPEND_THREADS)
+            if (p.b.group_start[i] <= r && r < p.b.group_start[i + 1]) grp_s = i;
+        __syncthreads();
+        grp = grp_s;
+    } else {
+        grp = r / p.b.uniform;
+        if (grp >= p.b.n_groups) grp = -1;
+    }
+    if (grp < 0) return;                                   // behind the last group
+    const long long row0 = pos < pg_pos_limit(p.b, p.ge) ? pg_row_of(p.b, p.ge, grp, 0, pos) : -1;
+    if (row0 < 0) {
+        if (threadIdx.x == 0) atomicOr(p.status, pos < pg_pos_limit(p.b, p.ge) ? PG_ST_BAD_PAGE : PG_ST_BAD_ROW);
+        return;
+    }
+    T* kd = (T*)p.k + (size_t)row0 * D;
+    T* vd = (T*)p.v + (size_t)row0 * D;
+    const size_t head = (size_t)D << p.ge.page_shift;      // elements between a page's heads
+    T* qd = (T*)p.q_out + (size_t)r * p.ldqo;
+    const float2* cs = p.cs ? p.cs + (size_t)pos * (D / 2) : nullptr;
+    constexpr int U = 4;
+    for (int c0 = blockIdx.y * PG_APPEND_THREADS + threadIdx.x; c0 < items; c0 += U * stride) {
+        float x[U][VEC];
+        int hd[U], e[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int c = c0 + u * stride;
+            hd[u] = -1;
+            if (c < items) {
+                hd[u] = c / per_head;
+                e[u] = (c - hd[u] * per_head) * VEC;
+                const int what = hd[u] < p.ge.n_heads ? 0 : hd[u] < p.ge.n_heads + p.ge.n_kv ? 1 : 2;
+                src.template load<VEC>(what, r, (hd[u] - (what == 0 ? 0 : what == 1 ? p.ge.n_heads : p.ge.n_heads + p.ge.n_kv)) * D + e[u], x[u]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (hd[u] < 0) continue;
+            T* dst;
+            bool turn = cs != nullptr;
+            if (hd[u] < p.ge.n_heads) dst = qd + (size_t)hd[u] * D + e[u];
+            else if (hd[u] < p.ge.n_heads + p.ge.n_kv) dst = kd + (size_t)(hd[u] - p.ge.n_heads) * head + e[u];
+            else { dst = vd + (size_t)(hd[u] - p.ge.n_heads - p.ge.n_kv) * head + e[u]; turn = false; }
+            PgVec<T, VEC> o;
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) {
+                float a = x[u][i], b = x[u][i + 1];
+                if (turn) {
+                    const float2 t = cs[(e[u] + i) / 2];
+                    const float y = a * t.x - b * t.y;
+                    b = a * t.y + b * t.x;
+                    a = y;
+                }
+                o.x[i] = pg_from_f<T>(a);
+                o.x[i + 1] = pg_from_f<T>(b);
+            }
+            *reinterpret_cast<PgVec<T, VEC>*>(dst) = o;
+        }
+    }
+}
+
+}  // namespace rd

@@ -1,0 +1,479 @@
+// Attention over a paged cache for many rows per sequence (prompts, slices of prompts, wide wavefronts of
+// grouped heads), bf16, on the 5th-generation tensor cores.
+//
+// A row tile is 256 packed rows (two blocks A and B of 128), a key tile 128 positions.  Per key tile and block of
+// rows the tensor core does S = Q K^T and O += P V (2 x 128 x 128 x D MACs each, about 1,024 cycles at head_dim
+// 128) and the softmax 16,384 exponentials (about 1,024 cycles of the SM's 16 per cycle): the two take turns,
+// A's softmax under B's products and the other way round.
+//   warps 0-3 / 4-7  softmax of A / B: one packed row per thread (TMEM lane = row); S from TMEM to registers, mask,
+//                    online softmax in float32, P (bf16) back into the columns S came from
+//   warp 8           walks the block's share (rd_paged.cuh) and fills a ring of K and V tiles by TMA, one box per
+//                    page piece; it runs ahead across items
+//   warp 9           issues the MMAs: S_A(0) S_B(0), then PV_A(j) S_A(j+1) PV_B(j) S_B(j+1); P is the A operand
+//                    from TMEM, V the MN-major B operand as it lies in its page
+// TMEM: S/P of A and B (128 columns each), O of A and B (D columns each).  MMAs complete in the order they are
+// issued, so the arrival of S(j+1) also says that P V(j) is done: a thread may then move its row's maximum and
+// rescale O in place.  The maximum moves only when a tile exceeds it by more than 2^8 (P stays below 256; the
+// result does not depend on which maximum was used).
+// P is rounded to bf16 (the operand type); sums, maxima and O are float32.
+// Keys some rows do not see: as in rd_paged_mma.cuh (P = 0, non-finite elements of V are taken out of the tile in
+// shared memory and given to the rows that see them at the end).
+// Every wait is bounded; on time-out the roles leave their loops, the copies in flight land, TMEM is freed and the
+// status word raised.  No role ever waits at a block barrier between the first and the last.
+#pragma once
+#include "rd_attn_tc.cuh"
+#include "rd_paged_mma.cuh"
+
+namespace rd {
+
+constexpr int PGT_KT = 128, PGT_M = 256;
+constexpr int PGT_THREADS = 384;           // two warpgroups of softmax, one for the other roles (register split)
+constexpr int PGT_QUEUE = 3;
+
+template <int D> struct PgtCfg {
+    static constexpr int NA = D / 64, NB = (D % 64) / 32;
+    static constexpr int A_BYTES = 128 * 128, B_BYTES = 128 * 64;        // 128 rows of 64 / 32 columns
+    static constexpr int TILE = NA * A_BYTES + NB * B_BYTES;
+    static constexpr int STAGES = D == 128 ? 5 : D == 96 ? 7 : 10;
+    static constexpr int SMEM = 1024 + 2 * TILE + STAGES * TILE;
+    static constexpr int S_COL = 0, O_COL = 256;                         // + 128 for block B
+};
+
+__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr) : "memory");
+}
+// Waits for the loads issued so far; the registers are operands so that no use of them moves in front of it.
+__device__ __forceinline__ void tmem_ld32_wait(uint32_t* v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+          "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]),
+          "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
+          "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]) :: "memory");
+}
+__device__ __forceinline__ void tmem_st32_issue(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+          "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]),
+          "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]),
+          "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D += A B with A in TMEM (row = lane, two bf16 of k per column), B from shared memory
+__device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// MN-major operand of several 64-column blocks, `apart` bytes from one to the next (128-byte swizzle)
+__device__ __forceinline__ uint64_t umma_desc_mn128_blocks(uint32_t saddr, uint32_t apart) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(apart >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+template <int D>
+__global__ void __launch_bounds__(PGT_THREADS, 1)
+pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ PgMaps maps) {
+    using C = PgtCfg<D>;
+    constexpr int S = C::STAGES, M = PGT_M, KT = PGT_KT;
+    extern __shared__ uint8_t pgt_raw[];
+    uint8_t* Qs = (uint8_t*)(((uintptr_t)pgt_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* ring = Qs + 2 * C::TILE;
+    __shared__ PgPlanSmem<1> plan;
+    __shared__ uint64_t full[S], empty[S], qu_full[PGT_QUEUE], qu_empty[PGT_QUEUE];
+    __shared__ uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+    __shared__ PgPiece queue[PGT_QUEUE];
+    __shared__ int found[PGT_QUEUE];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_s;
+    volatile int* abort_flag = &abort_s;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < S; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < PGT_QUEUE; s++) { mbar_init(&qu_full[s], 1); mbar_init(&qu_empty[s], 9); }
+        for (int w = 0; w < 2; w++) { mbar_init(&q_full[w], 4); mbar_init(&s_full[w], 1); mbar_init(&p_full[w], 4); mbar_init(&o_full[w], 1); }
+        abort_s = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 9) tmem_alloc(&tmem_slot, 512);
+    pdl_enter();
+    tc_fence_before();
+    pg_plan_share<PGT_THREADS, PGT_KT>(p, M, plan);
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    if (warp >= 8) {
+        pg_regs_less<PG_REGS_LESS>();
+        if (warp == 8) {
+        // ---- producer: K(0) V(0) K(1) V(1) ... of every piece ----
+        const int br = min(1 << p.ge.page_shift, KT), nbox = KT / br;
+        const int no_row = 0x7fffff00;
+        PgWalk walk;
+        walk.start(p, plan);
+        PgPiece pc;
+        int cnt = 0, qn = 0;
+        bool more = true, ok = true, bad = false;
+        while (more && ok) {
+            more = walk.next(p.ge.n_kv, &pc);
+            const int qs = qn % PGT_QUEUE;
+            if (qn >= PGT_QUEUE) ok = mbar_wait(&qu_empty[qs], ((qn / PGT_QUEUE) - 1) & 1);
+            if (!ok) break;
+            if (lane == 0) {
+                if (!more) pc.i1 = -1;
+                queue[qs] = pc;
+                found[qs] = 0;
+                mbar_arrive(&qu_full[qs]);
+            }
+            qn++;
+            if (!more) break;
+            const PgSpan span = pg_span<KT>(pc.pmin, pc.pmax, p.window, p.sinks);
+            for (int i = pc.i0; i < pc.i1 && ok; i++) {
+                const int key = pg_tile_key(span, i, KT) + lane * br;
+                int y = no_row;
+                if (lane < nbox && key <= pc.pmax) {
+                    const long long row = pg_row_of(p.b, p.ge, pc.grp, pc.head, key);
+                    if (row >= 0) y = (int)row;
+                    else if (p.window <= 0 || key < p.sinks || key + br > pc.pmin - p.window + 1) bad = true;
+                }
+                for (int kv = 0; kv < 2; kv++, cnt++) {
+                    const int s = cnt % S;
+                    if (cnt >= S) ok = mbar_wait(&empty[s], ((cnt / S) - 1) & 1);
+                    if (!ok || *abort_flag) { ok = false; break; }
+                    if (lane == 0) mbar_expect_tx(&full[s], C::TILE);
+                    __syncwarp();
+                    if (lane < nbox) {
+                        uint8_t* d = ring + s * C::TILE;
+#pragma unroll
+                        for (int a = 0; a < C::NA; a++)
+                            tma_load_2d(d + a * C::A_BYTES + lane * br * 128, kv ? &maps.v64 : &maps.k64, a * 64, y, &full[s]);
+                        if (C::NB) tma_load_2d(d + C::NA * C::A_BYTES + lane * br * 64, kv ? &maps.v32 : &maps.k32, C::NA * 64, y, &full[s]);
+                    }
+                }
+            }
+        }
+        if (!ok) *abort_flag = 1;
+        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.w.status, PG_ST_BAD_PAGE);
+        if (*abort_flag)
+            for (int c = max(0, cnt - S); c < cnt; c++) mbar_wait(&full[c % S], (c / S) & 1);
+        } else if (warp == 9) {
+        // ---- MMA issuer ----
+        constexpr uint32_t idesc_s = umma_idesc(KT);
+        constexpr uint32_t idesc_o = umma_idesc_bmn(C::NB ? 64 * C::NA : D);
+        constexpr uint32_t idesc_o32 = umma_idesc_bmn(32);
+        const uint32_t q0 = smem_u32(Qs), r0 = smem_u32(ring);
+        int cnt = 0;
+        uint32_t np[2] = {0, 0}, ns = 0;                   // P tiles consumed per block, pieces seen
+        bool ok = true;
+        for (int qn = 0; ok; qn++) {
+            const int qs = qn % PGT_QUEUE;
+            ok = !*abort_flag && mbar_wait(&qu_full[qs], (qn / PGT_QUEUE) & 1);
+            if (!ok) break;
+            const PgPiece pc = queue[qs];
+            if (pc.i1 < 0) break;
+            const int len = pc.i1 - pc.i0;
+            const int nb = (long long)pc.n * p.ge.g - (long long)pc.rt * M > 128 ? 2 : 1;
+            auto qk = [&](int w, int c) {                  // S_w = Q_w K^T, K in load number c
+                const uint32_t k0 = r0 + (c % S) * C::TILE, qw = q0 + w * C::TILE, d = tmem + C::S_COL + w * 128;
+                tc_fence_after();
+#pragma unroll
+                for (int a = 0; a < C::NA; a++)
+#pragma unroll
+                    for (int k = 0; k < 4; k++)
+                        umma_bf16(d, umma_desc_k128(qw + a * C::A_BYTES) + (uint64_t)(k * 2),
+                                  umma_desc_k128(k0 + a * C::A_BYTES) + (uint64_t)(k * 2), idesc_s, (a | k) ? 1u : 0u);
+                if (C::NB) {
+#pragma unroll
+                    for (int k = 0; k < 2; k++)
+                        umma_bf16(d, umma_desc_k64(qw + C::NA * C::A_BYTES) + (uint64_t)(k * 2),
+                                  umma_desc_k64(k0 + C::NA * C::A_BYTES) + (uint64_t)(k * 2), idesc_s, 1u);
+                }
+            };
+            auto pv = [&](int w, int c, bool first) {      // O_w += P_w V, V in load number c
+                const uint32_t v0 = r0 + (c % S) * C::TILE, a0 = tmem + C::S_COL + w * 128, d = tmem + C::O_COL + w * 128;
+                tc_fence_after();
+#pragma unroll
+                for (int k = 0; k < KT / 16; k++)
+                    umma_bf16_ts(d, a0 + k * 8, umma_desc_mn128_blocks(v0 + k * 2048, C::A_BYTES), idesc_o, (!first || k) ? 1u : 0u);
+                if (C::NB) {
+#pragma unroll
+                    for (int k = 0; k < KT / 16; k++)
+                        umma_bf16_ts(d + C::NA * 64, a0 + k * 8, umma_desc_mn64(v0 + C::NA * C::A_BYTES + k * 1024), idesc_o32, (!first || k) ? 1u : 0u);
+                }
+            };
+            if (lane == 0) {
+                ok = mbar_wait(&full[cnt % S], (cnt / S) & 1);
+                for (int w = 0; w < nb && ok; w++) {
+                    ok = !*abort_flag && mbar_wait(&q_full[w], ns & 1);
+                    if (!ok) break;
+                    qk(w, cnt);
+                    umma_commit(&s_full[w]);
+                }
+                if (ok) umma_commit(&empty[cnt % S]);      // K(0)
+                for (int j = 0; j < len && ok; j++) {
+                    const int cv = cnt + 2 * j + 1, ck = cv + 1;
+                    if (!mbar_wait(&full[cv % S], (cv / S) & 1)) { ok = false; break; }
+                    if (j + 1 < len && !mbar_wait(&full[ck % S], (ck / S) & 1)) { ok = false; break; }
+                    for (int w = 0; w < nb; w++) {
+                        if (*abort_flag || !mbar_wait(&p_full[w], np[w] & 1)) { ok = false; break; }
+                        np[w]++;
+                        pv(w, cv, j == 0);
+                        if (w == nb - 1) umma_commit(&empty[cv % S]);
+                        if (j + 1 < len) {
+                            qk(w, ck);
+                            umma_commit(&s_full[w]);
+                            if (w == nb - 1) umma_commit(&empty[ck % S]);
+                        } else {
+                            umma_commit(&o_full[w]);
+                        }
+                    }
+                }
+                if (!ok) *abort_flag = 1;
+            }
+            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+            __syncwarp();
+            cnt += 2 * len;
+            ns++;
+            if (lane == 0) mbar_arrive(&qu_empty[qs]);
+        }
+        if (!ok) *abort_flag = 1;
+        }
+    } else {
+        // ---- softmax ----
+        pg_regs_more<PG_REGS_MORE>();
+        const int w = warp >> 2, quad = warp & 3, rl = quad * 32 + lane;      // row of the block of 128
+        const uint32_t t_lane = tmem + ((uint32_t)(quad * 32) << 16);
+        const uint32_t t_s = t_lane + C::S_COL + w * 128, t_o = t_lane + C::O_COL + w * 128;
+        const int limit = pg_pos_limit(p.b, p.ge);
+        const float c2 = p.scale_log2;
+        uint32_t n_s = 0, n_o = 0;
+        int cnt = 0;
+        bool ok = true;
+        for (int qn = 0; ok; qn++) {
+            const int qs = qn % PGT_QUEUE;
+            ok = !*abort_flag && mbar_wait(&qu_full[qs], (qn / PGT_QUEUE) & 1);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const PgPiece pc = queue[qs];
+            if (pc.i1 < 0) break;
+            const PgSpan span = pg_span<KT>(pc.pmin, pc.pmax, p.window, p.sinks);
+            const int len = pc.i1 - pc.i0;
+            const long long packed = (long long)pc.n * p.ge.g;
+            const long long pk = (long long)pc.rt * M + w * 128 + rl;
+            const bool have = pk < packed;
+            const int row = have ? pc.a + (int)(pk / p.ge.g) : 0, hd = pc.head * p.ge.g + (have ? (int)(pk % p.ge.g) : 0);
+            int pos = have ? p.b.row_pos[row] : -1;
+            if (pos >= limit) pos = -1;
+            if (w == 1 && packed - (long long)pc.rt * M <= 128) {             // block B is empty
+                cnt += 2 * len;
+                __syncwarp();
+                if (lane == 0) { mbar_arrive(&q_full[1]); mbar_arrive(&qu_empty[qs]); }
+                continue;
+            }
+            {   // this row's query into the block's operand tile
+                const __nv_bfloat16* qr = (const __nv_bfloat16*)p.q + (size_t)row * p.ldq + (size_t)hd * D;
+                uint8_t* qd = Qs + w * C::TILE;
+#pragma unroll
+                for (int c = 0; c < D / 8; c++) {
+                    const uint4 v = have ? *reinterpret_cast<const uint4*>(qr + c * 8) : make_uint4(0, 0, 0, 0);
+                    uint8_t* d;
+                    if (c < 8 * C::NA) d = qd + (c >> 3) * C::A_BYTES + rl * 128 + (((c & 7) ^ (rl & 7)) << 4);
+                    else d = qd + C::NA * C::A_BYTES + rl * 64 + (((c & 3) ^ ((rl >> 1) & 3)) << 4);
+                    *reinterpret_cast<uint4*>(d) = v;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&q_full[w]);
+            }
+            float m = -INFINITY, l = 0.f;                  // m: the maximum (log2 domain) the row's P and O are scaled by
+            for (int j = 0; j < len; j++) {
+                ok = !*abort_flag && mbar_wait(&s_full[w], n_s & 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                n_s++;
+                tc_fence_after();
+                uint32_t sr[KT];
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) tmem_ld32_issue(t_s + c, sr + c);
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) tmem_ld32_wait(sr + c);
+                const int key0 = pg_tile_key(span, pc.i0 + j, KT);
+                const bool partial = pg_partial<KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks);
+                if (partial) {
+#pragma unroll
+                    for (int k = 0; k < KT; k++)
+                        if (!pg_sees(pos, key0 + k, p.window, p.sinks)) sr[k] = 0xff800000u;      // -inf
+                }
+                float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int k = 0; k < KT; k++) mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(sr[k]));
+                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * c2;
+                const bool move = mx > m + 8.0f || (m == -INFINITY && mx > -INFINITY);
+                if (__any_sync(0xffffffffu, move && l > 0.f)) {
+                    // O is at rest: the commit that announced S(j) covers P V(j - 1)
+                    const float corr = move ? ex2_approx(m - mx) : 1.0f;
+#pragma unroll
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t orow[32];
+                        tmem_ld32(t_o + c, orow);
+#pragma unroll
+                        for (int k = 0; k < 32; k++) orow[k] = __float_as_uint(__uint_as_float(orow[k]) * corr);
+                        tmem_st32(t_o + c, orow);
+                    }
+                    l *= corr;
+                }
+                if (move) m = mx;
+                const float u = m == -INFINITY ? 0.f : m;
+                float sum4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    uint32_t pw[32];
+#pragma unroll
+                    for (int k = 0; k < 32; k++) {
+                        const float p0 = ex2_approx(fmaf(__uint_as_float(sr[h * 64 + 2 * k]), c2, -u));
+                        const float p1 = ex2_approx(fmaf(__uint_as_float(sr[h * 64 + 2 * k + 1]), c2, -u));
+                        sum4[(2 * k) & 3] += p0;
+                        sum4[(2 * k + 1) & 3] += p1;
+                        pw[k] = pack_bf16(p0, p1);
+                    }
+                    tmem_st32_issue(t_s + h * 32, pw);
+                }
+                l += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+                if (partial && w == 0) {
+                    // thread = key: take non-finite elements out of this V tile before anyone multiplies by it
+                    const int cv = cnt + 2 * j + 1;
+                    ok = __all_sync(0xffffffffu, mbar_wait(&full[cv % S], (cv / S) & 1));
+                    if (!ok) break;
+                    uint8_t* vt = ring + (cv % S) * C::TILE;
+                    bool hit = false;
+#pragma unroll
+                    for (int c = 0; c < D / 8; c++) {
+                        uint8_t* d;
+                        if (c < 8 * C::NA) d = vt + (c >> 3) * C::A_BYTES + rl * 128 + (((c & 7) ^ (rl & 7)) << 4);
+                        else d = vt + C::NA * C::A_BYTES + rl * 64 + (((c & 3) ^ ((rl >> 1) & 3)) << 4);
+                        uint4 v = *reinterpret_cast<uint4*>(d);
+                        bool here = false;
+                        v.x = pgm_finite(v.x, &here); v.y = pgm_finite(v.y, &here); v.z = pgm_finite(v.z, &here); v.w = pgm_finite(v.w, &here);
+                        if (here) { *reinterpret_cast<uint4*>(d) = v; hit = true; }
+                    }
+                    if (hit) { *(volatile int*)&found[qs] = 1; __threadfence_block(); }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[w]);
+            }
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&o_full[w], n_o & 1));
+            n_o++;
+            cnt += 2 * len;
+            if (!ok) { *abort_flag = 1; break; }
+            tc_fence_after();
+            const bool whole = pc.c_first == pc.c_last, fix = *(volatile int*)&found[qs] != 0;
+            const bool real = pos >= 0;
+            float* slot = whole ? nullptr : pg_slot(p.w, blockIdx.x, pc.c_first, M, D);
+            const int rm = w * 128 + rl;
+            const float inv = 1.0f / l;
+            __nv_bfloat16* dst = (__nv_bfloat16*)p.out + (size_t)row * p.ldo + (size_t)hd * D;
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                uint32_t orow[32];
+                __syncwarp();                              // the load is the whole warp's
+                tmem_ld32(t_o + c, orow);
+                if (fix && real) {
+#pragma unroll 1
+                    for (int k = 0; k < 32; k++) {
+                        const float add = pg_nonfinite<KT>(p, pc, pos, c + k);
+#pragma unroll
+                        for (int k2 = 0; k2 < 32; k2++)
+                            if (k2 == k) orow[k2] = __float_as_uint(__uint_as_float(orow[k2]) + add);
+                    }
+                }
+                if (real && whole) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8) {
+                        uint32_t x[4];
+#pragma unroll
+                        for (int q = 0; q < 4; q++) x[q] = pack_bf16(__uint_as_float(orow[k + 2 * q]) * inv, __uint_as_float(orow[k + 2 * q + 1]) * inv);
+                        *reinterpret_cast<uint4*>(dst + c + k) = make_uint4(x[0], x[1], x[2], x[3]);
+                    }
+                } else if (real) {
+                    // slot layout of this kernel: [D / 4][256 rows][4], then (m, l) [256][2]
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        *reinterpret_cast<uint4*>(slot + ((size_t)((c + k) / 4) * M + rm) * 4) = make_uint4(orow[k], orow[k + 1], orow[k + 2], orow[k + 3]);
+                }
+            }
+            if (whole) {
+                if (real && p.lse) p.lse[(size_t)row * p.ge.n_heads + hd] = (m + log2f(l)) * 0.6931471805599453f;
+            } else {
+                if (real) *reinterpret_cast<float2*>(slot + (size_t)M * D + 2 * rm) = make_float2(m, l);
+                // a warp's 32 rows are joined by the warp that arrives last with them; no block waits for another
+                __threadfence();
+                __syncwarp();
+                int last = 0;
+                if (lane == 0) {
+                    int* ctr = p.w.counter + pc.c_first * 8 + warp;
+                    last = atomicAdd(ctr, 1) == pc.c_last - pc.c_first;
+                    if (last) atomicExch(ctr, 0);
+                    __threadfence();
+                }
+                last = __shfl_sync(0xffffffffu, last, 0);
+                if (last) {
+                    __threadfence();
+                    const int nseg = pc.c_last - pc.c_first + 1;
+                    if (real) {
+                        float mm = -INFINITY, den = 0.f;
+                        for (int s = 0; s < nseg; s++) mm = fmaxf(mm, __ldcg(pg_slot(p.w, pc.c_first + s, pc.c_first, M, D) + (size_t)M * D + 2 * rm));
+                        for (int s = 0; s < nseg; s++) {
+                            const float2 ml = __ldcg(reinterpret_cast<const float2*>(pg_slot(p.w, pc.c_first + s, pc.c_first, M, D) + (size_t)M * D + 2 * rm));
+                            den = fmaf(ml.y, ml.x == -INFINITY ? 0.f : exp2f(ml.x - mm), den);
+                        }
+                        const float iv = 1.0f / den;
+#pragma unroll 2
+                        for (int c = 0; c < D; c += 8) {
+                            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+                            for (int s = 0; s < nseg; s++) {
+                                const float* sl = pg_slot(p.w, pc.c_first + s, pc.c_first, M, D);
+                                const float ms = __ldcg(sl + (size_t)M * D + 2 * rm), f = ms == -INFINITY ? 0.f : exp2f(ms - mm);
+                                const float4 x = __ldcg(reinterpret_cast<const float4*>(sl + ((size_t)(c / 4) * M + rm) * 4));
+                                const float4 y = __ldcg(reinterpret_cast<const float4*>(sl + ((size_t)(c / 4 + 1) * M + rm) * 4));
+                                acc[0] = fmaf(x.x, f, acc[0]); acc[1] = fmaf(x.y, f, acc[1]); acc[2] = fmaf(x.z, f, acc[2]); acc[3] = fmaf(x.w, f, acc[3]);
+                                acc[4] = fmaf(y.x, f, acc[4]); acc[5] = fmaf(y.y, f, acc[5]); acc[6] = fmaf(y.z, f, acc[6]); acc[7] = fmaf(y.w, f, acc[7]);
+                            }
+                            uint32_t x[4];
+#pragma unroll
+                            for (int q = 0; q < 4; q++) x[q] = pack_bf16(acc[2 * q] * iv, acc[2 * q + 1] * iv);
+                            *reinterpret_cast<uint4*>(dst + c) = make_uint4(x[0], x[1], x[2], x[3]);
+                        }
+                        if (p.lse) p.lse[(size_t)row * p.ge.n_heads + hd] = (mm + log2f(den)) * 0.6931471805599453f;
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&qu_empty[qs]);
+        }
+        if (!ok) *abort_flag = 1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (tid == 0 && abort_s) atomicOr(p.w.status, PG_ST_TIMEOUT);
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+}  // namespace rd
