@@ -11,9 +11,9 @@
 // its keys are those at least one of its rows sees, in tiles of KT keys: first the tiles of the sinks, then
 // those from the oldest key inside a window to the newest position.
 //
-// Division of the work.  Key tiles of all (row tile, kv head) items are numbered in one sequence and cut
-// into one equal contiguous share per block, whatever the batch looks like: one sequence of 131,072
-// positions is split over all SMs, 64 ragged ones are packed onto them.  An item that lies in one share is
+// Division of the work.  The units of all (row tile, kv head) items - an item's fixed cost, then its key tiles -
+// are numbered in one sequence and cut into one equal contiguous share per block, whatever the batch looks
+// like: one sequence of 131,072 positions is split over all SMs, 64 ragged ones are packed onto them.  An item that lies in one share is
 // finished there; the shares of an item that is cut leave (maximum, sum, unnormalised output) in a workspace,
 // and the block that arrives last joins them in key order, so results do not depend on which block that is.
 #pragma once
@@ -65,7 +65,8 @@ struct PgAttend {
     float scale_log2;            // scale * log2(e)
     int packed_lo, packed_hi;    // groups with packed_lo < packed rows <= packed_hi are this launch's
     int inline_plan;             // every block makes the plan itself (few row tiles)
-    int min_share;               // key tiles a share has at least
+    int min_share;               // units a share has at least
+    int item_cost;               // units an item counts for besides its key tiles (its query, its output)
     int rec_cap;                 // row tiles the plan's array holds (more only come from a group_start that is not ascending)
 };
 
@@ -114,6 +115,13 @@ __device__ __forceinline__ bool pg_sees(int p, int j, int window, int sinks) {
 template <int KT> __device__ __forceinline__ bool pg_partial(int key0, int pmin, int pmax, int window, int sinks) {
     return key0 + KT - 1 > pmin || (window > 0 && pmax - key0 >= window && key0 + KT > sinks);
 }
+// The keys a row sees in 32 positions from key0 on, as bits: key0 + i <= pos, and i's key inside the window or a sink.
+// lo: oldest position inside the row's window (INT_MIN without one).
+__device__ __forceinline__ uint32_t pg_upto(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }   // lowest n bits
+__device__ __forceinline__ uint32_t pg_see_bits(int key0, int pos, int lo, int sinks) {
+    return pg_upto(pos + 1 - key0) & (~pg_upto(max(lo, key0) - key0) | pg_upto(sinks - key0));
+}
+__device__ __forceinline__ int pg_window_lo(int pos, int window) { return window > 0 ? pos - window + 1 : (int)0x80000000; }
 
 // ---- the plan -----------------------------------------------------------------------------------------------
 constexpr int PG_MAX_GROUPS = 4096;       // groups of a call
@@ -237,11 +245,12 @@ __global__ void __launch_bounds__(PG_PLAN_THREADS) pg_plan_kernel(const __grid_c
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.w.n_rec = n_rec;
 }
 
-// A block's share: units [u0, u1) of the numbered key tiles, and where u0 lies.
+// A block's share: units [u0, u1), and where u0 lies (unit `at` of the item: the fixed cost comes first).
 struct PgShare {
     long long u0, u1, per;
-    int rec, head, tile, n_rec;
+    int rec, head, at, n_rec;
 };
+__device__ __forceinline__ int pg_units(const PgAttend& p, int nt) { return nt > 0 ? nt + p.item_cost : 0; }
 template <int CAP> struct PgPlanSmem {
     PgRecord rec[CAP];           // CAP = PG_INLINE_REC, or 1 for a kernel whose plan is always made before it
     int first[CAP];
@@ -264,7 +273,7 @@ __device__ void pg_plan_share(const PgAttend& p, int M, PgPlanSmem<CAP>& sm) {
     }
     const int chunk = (n_rec + NT - 1) / NT, r0 = min(n_rec, (int)threadIdx.x * chunk), r1 = min(n_rec, r0 + chunk);
     long long mine = 0;
-    for (int r = r0; r < r1; r++) mine += rec[r].nt;
+    for (int r = r0; r < r1; r++) mine += pg_units(p, rec[r].nt);
     mine *= p.ge.n_kv;
     long long total;
     const long long before = pg_block_scan<NT, long long>(mine, sm.warp_sums, &total);
@@ -275,11 +284,12 @@ __device__ void pg_plan_share(const PgAttend& p, int M, PgPlanSmem<CAP>& sm) {
     if (u0 < u1 && u0 >= before && u0 < before + mine) {
         long long u = before;
         for (int r = r0; r < r1; r++) {
-            const long long len = (long long)rec[r].nt * p.ge.n_kv;
+            const int units = pg_units(p, rec[r].nt);
+            const long long len = (long long)units * p.ge.n_kv;
             if (u0 < u + len) {
                 sm.share.rec = r;
-                sm.share.head = (int)((u0 - u) / rec[r].nt);
-                sm.share.tile = (int)((u0 - u) % rec[r].nt);
+                sm.share.head = (int)((u0 - u) / units);
+                sm.share.at = (int)((u0 - u) % units);
                 break;
             }
             u += len;
@@ -296,33 +306,33 @@ struct PgPiece {
 // Walks a share piece by piece; every caller that walks (several warps may) sees the same pieces.
 struct PgWalk {
     long long u, u1, per;
-    int rec, head, tile, n_rec;
+    int rec, head, at, n_rec, cost;
     const PgRecord* recs;
     template <int CAP> __device__ __forceinline__ void start(const PgAttend& p, const PgPlanSmem<CAP>& sm) {
         u = sm.share.u0; u1 = sm.share.u1; per = sm.share.per;
-        rec = sm.share.rec; head = sm.share.head; tile = sm.share.tile; n_rec = sm.share.n_rec;
+        rec = sm.share.rec; head = sm.share.head; at = sm.share.at; n_rec = sm.share.n_rec; cost = p.item_cost;
         recs = CAP > 1 && p.inline_plan ? sm.rec : p.w.rec;
     }
     __device__ __forceinline__ bool next(int n_kv, PgPiece* o) {
-        if (u >= u1 || rec >= n_rec) return false;
-        PgRecord r = recs[rec];
-        while (r.nt == 0) {                       // row tiles without a row of a sequence
-            if (++rec >= n_rec) return false;
-            r = recs[rec];
+        while (u < u1 && rec < n_rec) {
+            const PgRecord r = recs[rec];
+            if (r.nt == 0) { rec++; continue; }       // a row tile without a row of a sequence
+            const int units = r.nt + cost, len = (int)min((long long)(units - at), u1 - u);
+            const int i0 = max(0, at - cost), i1 = at + len - cost;
+            const long long first = u - at + cost;    // unit of the item's first key tile
+            o->grp = r.grp; o->a = r.a; o->n = r.n; o->rt = r.rt; o->head = head;
+            o->i0 = i0; o->i1 = i1; o->nt = r.nt; o->pmin = r.pmin; o->pmax = r.pmax;
+            o->c_first = (int)(first / per);
+            o->c_last = (int)((first + r.nt - 1) / per);
+            u += len;
+            at += len;
+            if (at == units) {
+                at = 0;
+                if (++head == n_kv) { head = 0; rec++; }
+            }
+            if (i1 > i0) return true;                 // (a share may end inside an item's fixed cost)
         }
-        const int len = (int)min((long long)(r.nt - tile), u1 - u);
-        o->grp = r.grp; o->a = r.a; o->n = r.n; o->rt = r.rt; o->head = head;
-        o->i0 = tile; o->i1 = tile + len; o->nt = r.nt; o->pmin = r.pmin; o->pmax = r.pmax;
-        const long long first = u - tile;
-        o->c_first = (int)(first / per);
-        o->c_last = (int)((first + r.nt - 1) / per);
-        u += len;
-        tile += len;
-        if (tile == r.nt) {
-            tile = 0;
-            if (++head == n_kv) { head = 0; rec++; }
-        }
-        return true;
+        return false;
     }
 };
 

@@ -240,13 +240,15 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
                 const int key0 = pg_tile_key(span, pc.i0 + t, PGM_KT);
                 const bool partial = pg_partial<PGM_KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks);
                 if (partial) {
+                    const uint32_t see_a = pg_see_bits(key0, pos[0], pg_window_lo(pos[0], p.window), p.sinks);
+                    const uint32_t see_b = pg_see_bits(key0, pos[1], pg_window_lo(pos[1], p.window), p.sinks);
 #pragma unroll
                     for (int j = 0; j < PGM_KT / 8; j++) {
-                        const int k0 = key0 + j * 8 + 2 * tq;
-                        if (!pg_sees(pos[0], k0, p.window, p.sinks)) sc[j][0] = -INFINITY;
-                        if (!pg_sees(pos[0], k0 + 1, p.window, p.sinks)) sc[j][1] = -INFINITY;
-                        if (!pg_sees(pos[1], k0, p.window, p.sinks)) sc[j][2] = -INFINITY;
-                        if (!pg_sees(pos[1], k0 + 1, p.window, p.sinks)) sc[j][3] = -INFINITY;
+                        const int k0 = j * 8 + 2 * tq;
+                        sc[j][0] = (see_a >> k0 & 1) ? sc[j][0] : -INFINITY;
+                        sc[j][1] = (see_a >> k0 & 2) ? sc[j][1] : -INFINITY;
+                        sc[j][2] = (see_b >> k0 & 1) ? sc[j][2] : -INFINITY;
+                        sc[j][3] = (see_b >> k0 & 2) ? sc[j][3] : -INFINITY;
                     }
                 }
                 float mx_a = -INFINITY, mx_b = -INFINITY;

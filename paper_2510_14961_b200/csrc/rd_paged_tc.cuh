@@ -80,6 +80,13 @@ __device__ __forceinline__ uint64_t umma_desc_mn128_blocks(uint32_t saddr, uint3
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(apart >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
+// One lane of a converged warp, the same every time.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+
 template <int D>
 __global__ void __launch_bounds__(PGT_THREADS, 1)
 pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ PgMaps maps) {
@@ -211,25 +218,27 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                         umma_bf16_ts(d + C::NA * 64, a0 + k * 8, umma_desc_mn64(v0 + C::NA * C::A_BYTES + k * 1024), idesc_o32, (!first || k) ? 1u : 0u);
                 }
             };
-            if (lane == 0) {
-                ok = mbar_wait(&full[cnt % S], (cnt / S) & 1);
-                for (int w = 0; w < nb && ok; w++) {
-                    ok = !*abort_flag && mbar_wait(&q_full[w], ns & 1);
-                    if (!ok) break;
+            const bool issuer = elect_one();
+            ok = mbar_wait(&full[cnt % S], (cnt / S) & 1);
+            for (int w = 0; w < nb && ok; w++) {
+                ok = !*abort_flag && mbar_wait(&q_full[w], ns & 1);
+                if (ok && issuer) {
                     qk(w, cnt);
                     umma_commit(&s_full[w]);
+                    if (w == nb - 1) umma_commit(&empty[cnt % S]);      // K(0)
                 }
-                if (ok) umma_commit(&empty[cnt % S]);      // K(0)
-                for (int j = 0; j < len && ok; j++) {
-                    const int cv = cnt + 2 * j + 1, ck = cv + 1;
-                    if (!mbar_wait(&full[cv % S], (cv / S) & 1)) { ok = false; break; }
-                    if (j + 1 < len && !mbar_wait(&full[ck % S], (ck / S) & 1)) { ok = false; break; }
-                    for (int w = 0; w < nb; w++) {
-                        if (*abort_flag || !mbar_wait(&p_full[w], np[w] & 1)) { ok = false; break; }
-                        np[w]++;
+            }
+            for (int j = 0; j < len && ok; j++) {
+                const int cv = cnt + 2 * j + 1, ck = cv + 1;
+                const bool more = j + 1 < len;
+                ok = mbar_wait(&full[cv % S], (cv / S) & 1) && (!more || mbar_wait(&full[ck % S], (ck / S) & 1));
+                for (int w = 0; w < nb && ok; w++) {
+                    ok = !*abort_flag && mbar_wait(&p_full[w], np[w] & 1);
+                    np[w]++;
+                    if (ok && issuer) {
                         pv(w, cv, j == 0);
                         if (w == nb - 1) umma_commit(&empty[cv % S]);
-                        if (j + 1 < len) {
+                        if (more) {
                             qk(w, ck);
                             umma_commit(&s_full[w]);
                             if (w == nb - 1) umma_commit(&empty[ck % S]);
@@ -238,9 +247,9 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                         }
                     }
                 }
-                if (!ok) *abort_flag = 1;
             }
-            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) *abort_flag = 1;
             __syncwarp();
             cnt += 2 * len;
             ns++;
@@ -280,21 +289,32 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                 if (lane == 0) { mbar_arrive(&q_full[1]); mbar_arrive(&qu_empty[qs]); }
                 continue;
             }
-            {   // this row's query into the block's operand tile
-                const __nv_bfloat16* qr = (const __nv_bfloat16*)p.q + (size_t)row * p.ldq + (size_t)hd * D;
-                uint8_t* qd = Qs + w * C::TILE;
+            // the warp's 32 queries into the block's operand tile: D / 8 lanes share a row (whole lines from memory)
+            uint8_t* qd = Qs + w * C::TILE + quad * 32 * 128;      // (64-column sub-tiles; the 32-column one has rows of 64 bytes)
+            constexpr int CH = D / 8, RI = 32 / CH;                // 16-byte chunks of a row, rows per turn
+            const int ch = lane % CH, rr = lane / CH;
+            const uint32_t c_off = ch < 8 * C::NA ? (uint32_t)((ch >> 3) * C::A_BYTES) : (uint32_t)(C::NA * C::A_BYTES - quad * 32 * 64);
+            auto place = [&](int r) {                              // chunk `ch` of the warp's row r
+                return ch < 8 * C::NA ? qd + c_off + r * 128 + (((ch & 7) ^ (r & 7)) << 4) : qd + c_off + r * 64 + (((ch & 3) ^ ((r >> 1) & 3)) << 4);
+            };
+            {
+                const unsigned long long my = have ? (unsigned long long)((const __nv_bfloat16*)p.q + (size_t)row * p.ldq + (size_t)hd * D) : 0ull;
+uint4 x[(32 + RI - 1) / RI];                   // every load is under way before the first store
 #pragma unroll
-                for (int c = 0; c < D / 8; c++) {
-                    const uint4 v = have ? *reinterpret_cast<const uint4*>(qr + c * 8) : make_uint4(0, 0, 0, 0);
-                    uint8_t* d;
-                    if (c < 8 * C::NA) d = qd + (c >> 3) * C::A_BYTES + rl * 128 + (((c & 7) ^ (rl & 7)) << 4);
-                    else d = qd + C::NA * C::A_BYTES + rl * 64 + (((c & 3) ^ ((rl >> 1) & 3)) << 4);
-                    *reinterpret_cast<uint4*>(d) = v;
+                for (int i = 0; i < 32; i += RI) {
+                    const int r = i + rr;
+                    const unsigned long long src = __shfl_sync(0xffffffffu, my, r & 31);
+                    x[i / RI] = make_uint4(0, 0, 0, 0);
+                    if (rr < RI && r < 32 && src) x[i / RI] = __ldg(reinterpret_cast<const uint4*>(src) + ch);
                 }
+#pragma unroll
+                for (int i = 0; i < 32; i += RI)
+                    if (rr < RI && i + rr < 32) *reinterpret_cast<uint4*>(place(i + rr)) = x[i / RI];
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&q_full[w]);
             }
+            const int lo = pg_window_lo(pos, p.window);
             float m = -INFINITY, l = 0.f;                  // m: the maximum (log2 domain) the row's P and O are scaled by
             for (int j = 0; j < len; j++) {
                 ok = !*abort_flag && mbar_wait(&s_full[w], n_s & 1);
@@ -311,8 +331,11 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                 const bool partial = pg_partial<KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks);
                 if (partial) {
 #pragma unroll
-                    for (int k = 0; k < KT; k++)
-                        if (!pg_sees(pos, key0 + k, p.window, p.sinks)) sr[k] = 0xff800000u;      // -inf
+                    for (int c = 0; c < KT; c += 32) {
+                        const uint32_t see = pg_see_bits(key0 + c, pos, lo, p.sinks);
+#pragma unroll
+                        for (int k = 0; k < 32; k++) sr[c + k] = (see >> k & 1) ? sr[c + k] : 0xff800000u;      // -inf
+                    }
                 }
                 float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -355,16 +378,25 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                     ok = __all_sync(0xffffffffu, mbar_wait(&full[cv % S], (cv / S) & 1));
                     if (!ok) break;
                     uint8_t* vt = ring + (cv % S) * C::TILE;
+auto at = [&](int c) {
+                        return reinterpret_cast<uint4*>(c < 8 * C::NA ? vt + (c >> 3) * C::A_BYTES + rl * 128 + (((c & 7) ^ (rl & 7)) << 4)
+                                                                      : vt + C::NA * C::A_BYTES + rl * 64 + (((c & 3) ^ ((rl >> 1) & 3)) << 4));
+                    };
                     bool hit = false;
 #pragma unroll
                     for (int c = 0; c < D / 8; c++) {
-                        uint8_t* d;
-                        if (c < 8 * C::NA) d = vt + (c >> 3) * C::A_BYTES + rl * 128 + (((c & 7) ^ (rl & 7)) << 4);
-                        else d = vt + C::NA * C::A_BYTES + rl * 64 + (((c & 3) ^ ((rl >> 1) & 3)) << 4);
-                        uint4 v = *reinterpret_cast<uint4*>(d);
+                        const uint4 v = *at(c);
                         bool here = false;
-                        v.x = pgm_finite(v.x, &here); v.y = pgm_finite(v.y, &here); v.z = pgm_finite(v.z, &here); v.w = pgm_finite(v.w, &here);
-                        if (here) { *reinterpret_cast<uint4*>(d) = v; hit = true; }
+                        pgm_finite(v.x, &here); pgm_finite(v.y, &here); pgm_finite(v.z, &here); pgm_finite(v.w, &here);
+                        hit |= here;
+                    }
+                    if (hit) {
+#pragma unroll 1
+                        for (int c = 0; c < D / 8; c++) {
+                            uint4 v = *at(c);
+                            v.x = pgm_finite(v.x, &hit); v.y = pgm_finite(v.y, &hit); v.z = pgm_finite(v.z, &hit); v.w = pgm_finite(v.w, &hit);
+                            *at(c) = v;
+                        }
                     }
                     if (hit) { *(volatile int*)&found[qs] = 1; __threadfence_block(); }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -399,13 +431,17 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                             if (k2 == k) orow[k2] = __float_as_uint(__uint_as_float(orow[k2]) + add);
                     }
                 }
-                if (real && whole) {
+                if (whole) {
+                    // the block's queries are no longer needed (every S has been computed): their place takes the outputs
 #pragma unroll
                     for (int k = 0; k < 32; k += 8) {
                         uint32_t x[4];
 #pragma unroll
                         for (int q = 0; q < 4; q++) x[q] = pack_bf16(__uint_as_float(orow[k + 2 * q]) * inv, __uint_as_float(orow[k + 2 * q + 1]) * inv);
-                        *reinterpret_cast<uint4*>(dst + c + k) = make_uint4(x[0], x[1], x[2], x[3]);
+                        const int oc = (c + k) / 8;
+                        uint8_t* d = oc < 8 * C::NA ? qd + (oc >> 3) * C::A_BYTES + lane * 128 + (((oc & 7) ^ (lane & 7)) << 4)
+                                                    : qd + C::NA * C::A_BYTES - quad * 32 * 64 + lane * 64 + (((oc & 3) ^ ((lane >> 1) & 3)) << 4);
+                        *reinterpret_cast<uint4*>(d) = make_uint4(x[0], x[1], x[2], x[3]);
                     }
                 } else if (real) {
                     // slot layout of this kernel: [D / 4][256 rows][4], then (m, l) [256][2]
@@ -415,6 +451,14 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                 }
             }
             if (whole) {
+                __syncwarp();
+                const unsigned long long my = real ? (unsigned long long)dst : 0ull;
+#pragma unroll
+                for (int i = 0; i < 32; i += RI) {
+                    const int r = i + rr;
+                    const unsigned long long to = __shfl_sync(0xffffffffu, my, r & 31);
+                    if (rr < RI && r < 32 && to) *reinterpret_cast<uint4*>(to + ch * 16) = *reinterpret_cast<const uint4*>(place(r));
+                }
                 if (real && p.lse) p.lse[(size_t)row * p.ge.n_heads + hd] = (m + log2f(l)) * 0.6931471805599453f;
             } else {
                 if (real) *reinterpret_cast<float2*>(slot + (size_t)M * D + 2 * rm) = make_float2(m, l);
