@@ -156,7 +156,8 @@ extern "C" int rd_paged_create(const rd_paged_config* cfg, void* k_pages, void* 
     const double rows = (double)g.n_layers * g.n_pages * g.n_kv_heads * g.page_size;
     if (rows > 2147483647.0 - 512.0) return RD_E_CAPACITY;
     if (g.max_rows == 0) g.max_rows = 65536;
-    if (g.max_rows > (1 << 24)) return RD_E_CAPACITY;
+    // packed rows (rows x query heads per K/V head) are counted in 31 bits
+    if (g.max_rows > (1 << 24) || (double)g.max_rows * (g.n_heads / g.n_kv_heads) > 1e9) return RD_E_CAPACITY;
     rd_paged* c = new (std::nothrow) rd_paged();
     if (!c) return RD_E_OOM;
     c->cfg = g;
@@ -257,7 +258,7 @@ template <typename T> static int attend_simt_d(rd_paged* c, const PgAttend& a, b
 static int attend_part(rd_paged* c, PgAttend a, bool many, int m, cudaStream_t st, bool chained, int* launches) {
     if (c->tensor) {
         a.min_share = many ? 1 : 4;
-        a.item_cost = many ? 2 : 2;
+        a.item_cost = many ? 4 : 2;
         if (many) return a.ge.D == 64 ? attend_many_tensor<64>(c, a, st, chained, launches) : a.ge.D == 96 ? attend_many_tensor<96>(c, a, st, chained, launches)
                                                                                                 : attend_many_tensor<128>(c, a, st, chained, launches);
         return a.ge.D == 64 ? attend_few_tensor<64>(c, a, m, st, chained, launches) : a.ge.D == 96 ? attend_few_tensor<96>(c, a, m, st, chained, launches)

@@ -66,6 +66,12 @@ __device__ __forceinline__ void tmem_st32_issue(uint32_t taddr, const uint32_t* 
           "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]),
           "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
+__device__ __forceinline__ void tmem_st16_issue(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+          "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // D += A B with A in TMEM (row = lane, two bf16 of k per column), B from shared memory
 __device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -87,6 +93,42 @@ __device__ __forceinline__ bool elect_one() {
     return yes != 0;
 }
 
+// Two floats at once (the FMA pipe's packed forms).
+typedef unsigned long long pgt_f2;
+__device__ __forceinline__ pgt_f2 pgt_pack(float a, float b) { pgt_f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void pgt_unpack(pgt_f2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
+__device__ __forceinline__ pgt_f2 pgt_fma(pgt_f2 a, pgt_f2 b, pgt_f2 c) { pgt_f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ pgt_f2 pgt_add(pgt_f2 a, pgt_f2 b) { pgt_f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+// largest of three, NaN if one is (a NaN score has to reach its row)
+__device__ __forceinline__ float pgt_max3(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+
+// 2^x for two x <= 126 on the FMA and integer pipes: x = n + f with n the nearest whole number (adding 1.5 * 2^23
+// leaves it in the low bits) and |f| <= 1/2, 2^f by a polynomial, n added to its exponent.  The coefficients are a
+// minimax fit of 2^f with p(0) = 1 (largest relative error 2.9e-6, far below the rounding of P to bf16).  x is
+// held at -127, where the sum of the exponents is 0: everything below 2^-127, masked scores too, comes out as 0
+// (or less than 2^-126).  The softmax gives some of its exponentials to these pipes because 128 of them per
+// thread and tile keep the SM's MUFU busy for as long as the two products take.
+__device__ __forceinline__ void pgt_exp2_pair(pgt_f2 x, float* e0, float* e1) {
+    float a, b;
+    pgt_unpack(x, &a, &b);
+    x = pgt_pack(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
+    const pgt_f2 r = pgt_add(x, pgt_pack(12582912.0f, 12582912.0f));
+    const pgt_f2 n = pgt_add(r, pgt_pack(-12582912.0f, -12582912.0f));
+    const pgt_f2 f = pgt_fma(n, pgt_pack(-1.0f, -1.0f), x);
+    pgt_f2 p = pgt_fma(f, pgt_pack(0.009582853f, 0.009582853f), pgt_pack(0.055906426f, 0.055906426f));
+    p = pgt_fma(p, f, pgt_pack(0.24024099f, 0.24024099f));
+    p = pgt_fma(p, f, pgt_pack(0.6931242f, 0.6931242f));
+    p = pgt_fma(p, f, pgt_pack(1.0f, 1.0f));
+    float p0, p1, r0, r1;
+    pgt_unpack(p, &p0, &p1);
+    pgt_unpack(r, &r0, &r1);
+    *e0 = __int_as_float(__float_as_int(p0) + (__float_as_int(r0) << 23));
+    *e1 = __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23));
+}
+#ifndef PGT_POLY
+#define PGT_POLY 4                     // of this many pairs of exponentials one goes to the FMA pipe
+#endif
+
 template <int D>
 __global__ void __launch_bounds__(PGT_THREADS, 1)
 pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ PgMaps maps) {
@@ -97,7 +139,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
     uint8_t* ring = Qs + 2 * C::TILE;
     __shared__ PgPlanSmem<1> plan;
     __shared__ uint64_t full[S], empty[S], qu_full[PGT_QUEUE], qu_empty[PGT_QUEUE];
-    __shared__ uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+    __shared__ uint64_t q_full[2], s_full[2], p_lo[2], p_hi[2], o_full[2];     // P in two parts: 96 keys, 32 keys
     __shared__ PgPiece queue[PGT_QUEUE];
     __shared__ int found[PGT_QUEUE];
     __shared__ uint32_t tmem_slot;
@@ -108,7 +150,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
     if (tid == 0) {
         for (int s = 0; s < S; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int s = 0; s < PGT_QUEUE; s++) { mbar_init(&qu_full[s], 1); mbar_init(&qu_empty[s], 9); }
-        for (int w = 0; w < 2; w++) { mbar_init(&q_full[w], 4); mbar_init(&s_full[w], 1); mbar_init(&p_full[w], 4); mbar_init(&o_full[w], 1); }
+        for (int w = 0; w < 2; w++) { mbar_init(&q_full[w], 4); mbar_init(&s_full[w], 1); mbar_init(&p_lo[w], 4); mbar_init(&p_hi[w], 4); mbar_init(&o_full[w], 1); }
         abort_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -189,7 +231,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
             const PgPiece pc = queue[qs];
             if (pc.i1 < 0) break;
             const int len = pc.i1 - pc.i0;
-            const int nb = (long long)pc.n * p.ge.g - (long long)pc.rt * M > 128 ? 2 : 1;
+            const int nb = (unsigned)pc.n * p.ge.g - (unsigned)pc.rt * M > 128u ? 2 : 1;
             auto qk = [&](int w, int c) {                  // S_w = Q_w K^T, K in load number c
                 const uint32_t k0 = r0 + (c % S) * C::TILE, qw = q0 + w * C::TILE, d = tmem + C::S_COL + w * 128;
                 tc_fence_after();
@@ -206,15 +248,15 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                                   umma_desc_k64(k0 + C::NA * C::A_BYTES) + (uint64_t)(k * 2), idesc_s, 1u);
                 }
             };
-            auto pv = [&](int w, int c, bool first) {      // O_w += P_w V, V in load number c
+            auto pv = [&](int w, int c, bool first, int k0, int k1) {      // O_w += P_w V over keys 16 k0 .. 16 k1, V in load number c
                 const uint32_t v0 = r0 + (c % S) * C::TILE, a0 = tmem + C::S_COL + w * 128, d = tmem + C::O_COL + w * 128;
                 tc_fence_after();
 #pragma unroll
-                for (int k = 0; k < KT / 16; k++)
+                for (int k = k0; k < k1; k++)
                     umma_bf16_ts(d, a0 + k * 8, umma_desc_mn128_blocks(v0 + k * 2048, C::A_BYTES), idesc_o, (!first || k) ? 1u : 0u);
                 if (C::NB) {
 #pragma unroll
-                    for (int k = 0; k < KT / 16; k++)
+                    for (int k = k0; k < k1; k++)
                         umma_bf16_ts(d + C::NA * 64, a0 + k * 8, umma_desc_mn64(v0 + C::NA * C::A_BYTES + k * 1024), idesc_o32, (!first || k) ? 1u : 0u);
                 }
             };
@@ -233,10 +275,13 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                 const bool more = j + 1 < len;
                 ok = mbar_wait(&full[cv % S], (cv / S) & 1) && (!more || mbar_wait(&full[ck % S], (ck / S) & 1));
                 for (int w = 0; w < nb && ok; w++) {
-                    ok = !*abort_flag && mbar_wait(&p_full[w], np[w] & 1);
+                    ok = !*abort_flag && mbar_wait(&p_lo[w], np[w] & 1);
+                    if (ok && issuer) pv(w, cv, j == 0, 0, 6);
+                    __syncwarp();
+                    ok = ok && mbar_wait(&p_hi[w], np[w] & 1);
                     np[w]++;
                     if (ok && issuer) {
-                        pv(w, cv, j == 0);
+                        pv(w, cv, false, 6, 8);
                         if (w == nb - 1) umma_commit(&empty[cv % S]);
                         if (more) {
                             qk(w, ck);
@@ -277,13 +322,13 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
             if (pc.i1 < 0) break;
             const PgSpan span = pg_span<KT>(pc.pmin, pc.pmax, p.window, p.sinks);
             const int len = pc.i1 - pc.i0;
-            const long long packed = (long long)pc.n * p.ge.g;
-            const long long pk = (long long)pc.rt * M + w * 128 + rl;
+            const unsigned packed = (unsigned)pc.n * p.ge.g, pk = (unsigned)pc.rt * M + w * 128 + rl;     // (below 2^31: max_rows)
             const bool have = pk < packed;
-            const int row = have ? pc.a + (int)(pk / p.ge.g) : 0, hd = pc.head * p.ge.g + (have ? (int)(pk % p.ge.g) : 0);
+            const unsigned of = have ? pk / (unsigned)p.ge.g : 0u;
+            const int row = have ? pc.a + (int)of : 0, hd = pc.head * p.ge.g + (have ? (int)(pk - of * p.ge.g) : 0);
             int pos = have ? p.b.row_pos[row] : -1;
             if (pos >= limit) pos = -1;
-            if (w == 1 && packed - (long long)pc.rt * M <= 128) {             // block B is empty
+            if (w == 1 && packed - (unsigned)pc.rt * M <= 128u) {             // block B is empty
                 cnt += 2 * len;
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(&q_full[1]); mbar_arrive(&qu_empty[qs]); }
@@ -337,11 +382,15 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                         for (int k = 0; k < 32; k++) sr[c + k] = (see >> k & 1) ? sr[c + k] : 0xff800000u;      // -inf
                     }
                 }
-                float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                float mx4[4] = {__uint_as_float(sr[0]), __uint_as_float(sr[1]), __uint_as_float(sr[2]), __uint_as_float(sr[3])};
 #pragma unroll
-                for (int k = 0; k < KT; k++) mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(sr[k]));
-                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * c2;
-                const bool move = mx > m + 8.0f || (m == -INFINITY && mx > -INFINITY);
+                for (int k = 4; k + 8 <= KT; k += 8)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) mx4[q] = pgt_max3(mx4[q], __uint_as_float(sr[k + 2 * q]), __uint_as_float(sr[k + 2 * q + 1]));
+                mx4[0] = pgt_max3(mx4[0], __uint_as_float(sr[KT - 4]), __uint_as_float(sr[KT - 3]));
+                mx4[1] = pgt_max3(mx4[1], __uint_as_float(sr[KT - 2]), __uint_as_float(sr[KT - 1]));
+                const float mx = pgt_max3(pgt_max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]) * c2;
+                const bool move = !(mx <= m + 8.0f) || (m == -INFINITY && mx > -INFINITY);      // (a NaN moves it, too)
                 if (__any_sync(0xffffffffu, move && l > 0.f)) {
                     // O is at rest: the commit that announced S(j) covers P V(j - 1)
                     const float corr = move ? ex2_approx(m - mx) : 1.0f;
@@ -357,21 +406,6 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                 }
                 if (move) m = mx;
                 const float u = m == -INFINITY ? 0.f : m;
-                float sum4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    uint32_t pw[32];
-#pragma unroll
-                    for (int k = 0; k < 32; k++) {
-                        const float p0 = ex2_approx(fmaf(__uint_as_float(sr[h * 64 + 2 * k]), c2, -u));
-                        const float p1 = ex2_approx(fmaf(__uint_as_float(sr[h * 64 + 2 * k + 1]), c2, -u));
-                        sum4[(2 * k) & 3] += p0;
-                        sum4[(2 * k + 1) & 3] += p1;
-                        pw[k] = pack_bf16(p0, p1);
-                    }
-                    tmem_st32_issue(t_s + h * 32, pw);
-                }
-                l += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
                 if (partial && w == 0) {
                     // thread = key: take non-finite elements out of this V tile before anyone multiplies by it
                     const int cv = cnt + 2 * j + 1;
@@ -382,14 +416,14 @@ auto at = [&](int c) {
                         return reinterpret_cast<uint4*>(c < 8 * C::NA ? vt + (c >> 3) * C::A_BYTES + rl * 128 + (((c & 7) ^ (rl & 7)) << 4)
                                                                       : vt + C::NA * C::A_BYTES + rl * 64 + (((c & 3) ^ ((rl >> 1) & 3)) << 4));
                     };
-                    bool hit = false;
+                    uint32_t seen = 0;
 #pragma unroll
                     for (int c = 0; c < D / 8; c++) {
-                        const uint4 v = *at(c);
-                        bool here = false;
-                        pgm_finite(v.x, &here); pgm_finite(v.y, &here); pgm_finite(v.z, &here); pgm_finite(v.w, &here);
-                        hit |= here;
+                        const uint4 v = *at(c);        // an exponent of all ones carries into bit 15 (31)
+                        seen |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) |
+                                ((v.z & 0x7f807f80u) + 0x00800080u) | ((v.w & 0x7f807f80u) + 0x00800080u);
                     }
+                    bool hit = (seen & 0x80008000u) != 0;
                     if (hit) {
 #pragma unroll 1
                         for (int c = 0; c < D / 8; c++) {
@@ -401,10 +435,45 @@ auto at = [&](int c) {
                     if (hit) { *(volatile int*)&found[qs] = 1; __threadfence_block(); }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
+                const pgt_f2 cc = pgt_pack(c2, c2), uu = pgt_pack(-u, -u);
+                pgt_f2 sums[2] = {0ull, 0ull};
+                // P of 32 keys (16 packed words) from their scores
+                auto exps = [&](const uint32_t* s, uint32_t* pw) {
+#pragma unroll
+                    for (int k = 0; k < 16; k++) {
+                        const pgt_f2 x = pgt_fma(pgt_pack(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), cc, uu);
+                        float e0, e1;
+                        if (k % PGT_POLY == PGT_POLY - 1) {
+                            pgt_exp2_pair(x, &e0, &e1);
+                        } else {
+                            pgt_unpack(x, &e0, &e1);
+                            e0 = ex2_approx(e0);
+                            e1 = ex2_approx(e1);
+                        }
+                        sums[k & 1] = pgt_add(sums[k & 1], pgt_pack(e0, e1));
+                        pw[k] = pack_bf16(e0, e1);
+                    }
+                };
+                uint32_t pw[32];
+                exps(sr, pw);
+                exps(sr + 32, pw + 16);
+                tmem_st32_issue(t_s, pw);
+                exps(sr + 64, pw);
+                tmem_st16_issue(t_s + 32, pw);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[w]);
+                if (lane == 0) mbar_arrive(&p_lo[w]);      // the product may begin with these 96 keys
+                exps(sr + 96, pw);
+                tmem_st16_issue(t_s + 48, pw);
+                float s0, s1, s2, s3;
+                pgt_unpack(sums[0], &s0, &s1);
+                pgt_unpack(sums[1], &s2, &s3);
+                l += (s0 + s1) + (s2 + s3);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_hi[w]);
             }
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&o_full[w], n_o & 1));
             n_o++;
