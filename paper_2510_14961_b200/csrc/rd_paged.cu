@@ -257,7 +257,7 @@ template <typename T> static int attend_simt_d(rd_paged* c, const PgAttend& a, b
 }
 static int attend_part(rd_paged* c, PgAttend a, bool many, int m, cudaStream_t st, bool chained, int* launches) {
     if (c->tensor) {
-        a.min_share = many ? 1 : 4;
+        a.min_share = many ? 1 : 18;
         a.item_cost = many ? 4 : 2;
         if (many) return a.ge.D == 64 ? attend_many_tensor<64>(c, a, st, chained, launches) : a.ge.D == 96 ? attend_many_tensor<96>(c, a, st, chained, launches)
                                                                                                 : attend_many_tensor<128>(c, a, st, chained, launches);

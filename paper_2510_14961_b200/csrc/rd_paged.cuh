@@ -352,9 +352,9 @@ __device__ __forceinline__ float* pg_slot(const PgWork& w, int c, int c_first, i
 // in the block that arrives last, which then sees every slot.
 template <typename Sync>
 __device__ __forceinline__ bool pg_arrive_last(const PgWork& w, const PgPiece& pc, bool leader, int* flag, Sync sync) {
-    __threadfence();
-    sync();
+    sync();                                        // (the leader's fence covers what the barrier has ordered before it)
     if (leader) {
+        __threadfence();
         const int want = pc.c_last - pc.c_first;
         const int seen = atomicAdd(&w.counter[pc.c_first], 1);
         const bool last = seen == want;
@@ -363,9 +363,7 @@ __device__ __forceinline__ bool pg_arrive_last(const PgWork& w, const PgPiece& p
         __threadfence();
     }
     sync();
-    const bool last = *flag != 0;
-    if (last) __threadfence();
-    return last;
+    return *flag != 0;
 }
 __device__ __forceinline__ void pg_store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ __forceinline__ void pg_store4(__nv_bfloat16* p, float a, float b, float c, float d) {

@@ -27,7 +27,7 @@ namespace rd {
 
 constexpr int PGM_KT = 32;
 constexpr int PGM_THREADS = 384;           // two warpgroups of consumers, one for the producer (register split)
-constexpr int PGM_QUEUE = 4;               // pieces the producer may be ahead
+constexpr int PGM_QUEUE = 8;               // pieces known in advance
 
 struct PgMaps { CUtensorMap k64, k32, v64, v32; };   // boxes of min(page_size, KT) positions x 64 / 32 columns
 
@@ -87,6 +87,121 @@ __device__ float pg_nonfinite(const PgAttend& p, const PgPiece& pc, int pos, int
     return add;
 }
 
+// One lane of a converged warp, the same every time.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+
+// Two floats at once (the FMA pipe's packed forms).
+typedef unsigned long long pgt_f2;
+__device__ __forceinline__ pgt_f2 pgt_pack(float a, float b) { pgt_f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void pgt_unpack(pgt_f2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
+__device__ __forceinline__ pgt_f2 pgt_fma(pgt_f2 a, pgt_f2 b, pgt_f2 c) { pgt_f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ pgt_f2 pgt_add(pgt_f2 a, pgt_f2 b) { pgt_f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+// largest of three, NaN if one is (a NaN score has to reach its row)
+__device__ __forceinline__ float pgt_max3(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+
+// 2^x for two x <= 126 on the FMA and integer pipes: x = n + f with n the nearest whole number (adding 1.5 * 2^23
+// leaves it in the low bits) and |f| <= 1/2, 2^f by a polynomial, n added to its exponent.  The coefficients are a
+// minimax fit of 2^f with p(0) = 1 (largest relative error 2.9e-6, far below the rounding of P to bf16).  x is
+// held at -127, where the sum of the exponents is 0: everything below 2^-127, masked scores too, comes out as 0
+// (or less than 2^-126).  The softmax gives some of its exponentials to these pipes because 128 of them per
+// thread and tile keep the SM's MUFU busy for as long as the two products take.
+__device__ __forceinline__ void pgt_exp2_pair(pgt_f2 x, float* e0, float* e1) {
+    float a, b;
+    pgt_unpack(x, &a, &b);
+    x = pgt_pack(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
+    const pgt_f2 r = pgt_add(x, pgt_pack(12582912.0f, 12582912.0f));
+    const pgt_f2 n = pgt_add(r, pgt_pack(-12582912.0f, -12582912.0f));
+    const pgt_f2 f = pgt_fma(n, pgt_pack(-1.0f, -1.0f), x);
+    pgt_f2 p = pgt_fma(f, pgt_pack(0.009582853f, 0.009582853f), pgt_pack(0.055906426f, 0.055906426f));
+    p = pgt_fma(p, f, pgt_pack(0.24024099f, 0.24024099f));
+    p = pgt_fma(p, f, pgt_pack(0.6931242f, 0.6931242f));
+    p = pgt_fma(p, f, pgt_pack(1.0f, 1.0f));
+    float p0, p1, r0, r1;
+    pgt_unpack(p, &p0, &p1);
+    pgt_unpack(r, &r0, &r1);
+    *e0 = __int_as_float(__float_as_int(p0) + (__float_as_int(r0) << 23));
+    *e1 = __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23));
+}
+#ifndef PGT_POLY
+#define PGT_POLY 4                     // of this many pairs of exponentials one goes to the FMA pipe
+#endif
+
+// A producer warp's view of a share: it walks the pieces into a queue in shared memory, one ahead of the piece it
+// loads, and turns key tiles into pool rows.  The table is read 32 boxes at a time, one per lane, a chunk ahead of its use
+// (the first chunk of a piece while the piece before it is being loaded), so that no copy waits for a table entry.
+template <int KT, int DEPTH> struct PgProducer {
+    PgPiece* queue;                    // [DEPTH]; i1 < 0: no more pieces
+    uint64_t *full, *empty;            // [DEPTH]
+    int* found;                        // [DEPTH], cleared with every piece, or null
+    int br, nbox, tpc;                 // positions of a box, boxes of a tile, tiles of a chunk
+    int cur, ahead, first;             // pool rows of this lane's box: current chunk, next chunk, first chunk of the next piece
+    int at;                            // lane of the next tile's first box
+    int qn;                            // pieces pushed
+    bool bad;
+    PgWalk walk;
+    __device__ __forceinline__ int look(const PgAttend& p, const PgPiece& q, int i_first) {
+        const int lane = threadIdx.x & 31, i = i_first + lane / nbox;
+        int y = 0x7fffff00;            // beyond the pages: the box reads as zeros
+        if (i < q.i1) {
+            const int key = pg_tile_key(pg_span<KT>(q.pmin, q.pmax, p.window, p.sinks), i, KT) + (lane % nbox) * br;
+            if (key <= q.pmax) {
+                const long long row = pg_row_of(p.b, p.ge, q.grp, q.head, key);
+                if (row >= 0) y = (int)row;
+                else if (p.window <= 0 || key < p.sinks || key + br > q.pmin - p.window + 1) bad = true;      // a page some row needs
+            }
+        }
+        return y;
+    }
+    // the next piece (or the end) into the queue, and the rows of its first boxes; false: a wait ran out
+    __device__ __forceinline__ bool push(const PgAttend& p) {
+        PgPiece pc;
+        const bool more = walk.next(p.ge.n_kv, &pc);
+        const int s = qn % DEPTH;
+        if (qn >= DEPTH && !mbar_wait(&empty[s], ((qn / DEPTH) - 1) & 1)) return false;
+        if ((threadIdx.x & 31) == 0) {
+            if (!more) pc.i1 = -1;
+            queue[s] = pc;
+            if (found) found[s] = 0;
+            mbar_arrive(&full[s]);
+        }
+        __syncwarp();
+        qn++;
+        if (more) first = look(p, queue[s], queue[s].i0);
+        return true;
+    }
+    template <typename Plan> __device__ __forceinline__ bool start(const PgAttend& p, const Plan& plan) {
+        br = min(1 << p.ge.page_shift, KT);
+        nbox = KT / br;
+        tpc = 32 / nbox;
+        bad = false;
+        qn = 0;
+        walk.start(p, plan);
+        return push(p);
+    }
+    // begins the oldest piece that has not been loaded (null: none is left, or a wait ran out: *ok)
+    __device__ __forceinline__ const PgPiece* begin(const PgAttend& p, bool* ok) {
+        const PgPiece* q = &queue[(qn - 1) % DEPTH];
+        if (q->i1 < 0) return nullptr;
+        cur = first;
+        at = 0;
+        ahead = look(p, *q, q->i0 + tpc);
+        *ok = push(p);
+        return *ok ? q : nullptr;
+    }
+    // lane that holds the row of tile i's first box; tiles are asked for in order, from the piece's first
+    __device__ __forceinline__ int tile_lane(const PgAttend& p, const PgPiece* q, int i) {
+        if (at == 32) { cur = ahead; ahead = look(p, *q, i + tpc); at = 0; }
+        const int l = at;
+        at += nbox;
+        return l;
+    }
+    __device__ __forceinline__ int row(int lane) const { return __shfl_sync(0xffffffffu, cur, lane); }
+};
+
 template <int D, int WQ>
 __global__ void __launch_bounds__(PGM_THREADS, 1)
 pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ PgMaps maps) {
@@ -120,57 +235,40 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
         pg_regs_less<PG_REGS_LESS>();
         if (warp == 8) {
         // ---- producer ----
-        const int br = min(1 << p.ge.page_shift, PGM_KT), nbox = PGM_KT / br;
-        const int no_row = 0x7fffff00;                     // beyond the pages: the box reads as zeros
-        PgWalk walk;
-        walk.start(p, plan);
-        PgPiece pc;
-        int cnt = 0, qn = 0;
-        bool more = true, ok = true, bad = false;
-        while (more && ok) {
-            more = walk.next(p.ge.n_kv, &pc);
-            const int qs = qn % PGM_QUEUE;
-            if (qn >= PGM_QUEUE) ok = mbar_wait(&q_empty[qs], ((qn / PGM_QUEUE) - 1) & 1);
-            if (!ok) break;
-            if (lane == 0) {
-                if (!more) pc.i1 = -1;
-                queue[qs] = pc;
-                mbar_arrive(&q_full[qs]);
-            }
-            qn++;
-            if (!more) break;
-            const PgSpan span = pg_span<PGM_KT>(pc.pmin, pc.pmax, p.window, p.sinks);
-            for (int i = pc.i0; i < pc.i1; i++, cnt++) {
-                const int s = cnt % S;
-                const int key = pg_tile_key(span, i, PGM_KT) + lane * br;
-                // the page is looked up while the stage is still in use
-                int y = no_row;
-                if (lane < nbox && key <= pc.pmax) {
-                    const long long row = pg_row_of(p.b, p.ge, pc.grp, pc.head, key);
-                    if (row >= 0) y = (int)row;
-                    else if (p.window <= 0 || key < p.sinks || key + br > pc.pmin - p.window + 1) bad = true;
-                }
-                if (cnt >= S) ok = mbar_wait(&empty[s], ((cnt / S) - 1) & 1);
-                if (!ok || *abort_flag) { ok = false; break; }
-                if (lane == 0) mbar_expect_tx(&full[s], C::STAGE_BYTES);
-                __syncwarp();
-                if (lane < nbox) {
-                    uint8_t* kd = ring + s * C::STAGE_BYTES;
-                    uint8_t* vd = kd + T::BYTES;
+        PgProducer<PGM_KT, PGM_QUEUE> bx;
+        bx.queue = queue; bx.full = q_full; bx.empty = q_empty; bx.found = nullptr;
+        bool ok = bx.start(p, plan);
+        const bool issuer = elect_one();
+        int cnt = 0;
+        while (ok) {
+            const PgPiece* q = bx.begin(p, &ok);
+            if (!q) break;
+            const int i1 = q->i1;
+            for (int i = q->i0; i < i1; i++, cnt++) {
+                const int s = cnt % S, l0 = bx.tile_lane(p, q, i);
+                if (cnt >= S && !mbar_wait(&empty[s], ((cnt / S) - 1) & 1)) { ok = false; break; }
+                uint8_t* kd = ring + s * C::STAGE_BYTES;
+                uint8_t* vd = kd + T::BYTES;
+                if (issuer) mbar_expect_tx(&full[s], C::STAGE_BYTES);
+#pragma unroll 1
+                for (int b = 0; b < bx.nbox; b++) {
+                    const int y = bx.row(l0 + b), at = b * bx.br;
+                    if (issuer) {
 #pragma unroll
-                    for (int a = 0; a < T::NA; a++) {
-                        tma_load_2d(kd + a * T::A_BYTES + lane * br * 128, &maps.k64, a * 64, y, &full[s]);
-                        tma_load_2d(vd + a * T::A_BYTES + lane * br * 128, &maps.v64, a * 64, y, &full[s]);
-                    }
-                    if (T::NB) {
-                        tma_load_2d(kd + T::NA * T::A_BYTES + lane * br * 64, &maps.k32, T::NA * 64, y, &full[s]);
-                        tma_load_2d(vd + T::NA * T::A_BYTES + lane * br * 64, &maps.v32, T::NA * 64, y, &full[s]);
+                        for (int a = 0; a < T::NA; a++) {
+                            tma_load_2d(kd + a * T::A_BYTES + at * 128, &maps.k64, a * 64, y, &full[s]);
+                            tma_load_2d(vd + a * T::A_BYTES + at * 128, &maps.v64, a * 64, y, &full[s]);
+                        }
+                        if (T::NB) {
+                            tma_load_2d(kd + T::NA * T::A_BYTES + at * 64, &maps.k32, T::NA * 64, y, &full[s]);
+                            tma_load_2d(vd + T::NA * T::A_BYTES + at * 64, &maps.v32, T::NA * 64, y, &full[s]);
+                        }
                     }
                 }
             }
         }
         if (!ok) *abort_flag = 1;
-        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.w.status, PG_ST_BAD_PAGE);
+        if (__any_sync(0xffffffffu, bx.bad) && lane == 0) atomicOr(p.w.status, PG_ST_BAD_PAGE);
         if (*abort_flag)                                   // every copy lands before the block's memory is released
             for (int c = max(0, cnt - S); c < cnt; c++) mbar_wait(&full[c % S], (c / S) & 1);
         }

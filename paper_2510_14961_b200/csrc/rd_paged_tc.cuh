@@ -28,7 +28,7 @@ namespace rd {
 
 constexpr int PGT_KT = 128, PGT_M = 256;
 constexpr int PGT_THREADS = 384;           // two warpgroups of softmax, one for the other roles (register split)
-constexpr int PGT_QUEUE = 3;
+constexpr int PGT_QUEUE = 4;
 
 template <int D> struct PgtCfg {
     static constexpr int NA = D / 64, NB = (D % 64) / 32;
@@ -86,49 +86,6 @@ __device__ __forceinline__ uint64_t umma_desc_mn128_blocks(uint32_t saddr, uint3
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(apart >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-// One lane of a converged warp, the same every time.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t yes;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
-    return yes != 0;
-}
-
-// Two floats at once (the FMA pipe's packed forms).
-typedef unsigned long long pgt_f2;
-__device__ __forceinline__ pgt_f2 pgt_pack(float a, float b) { pgt_f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void pgt_unpack(pgt_f2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
-__device__ __forceinline__ pgt_f2 pgt_fma(pgt_f2 a, pgt_f2 b, pgt_f2 c) { pgt_f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ pgt_f2 pgt_add(pgt_f2 a, pgt_f2 b) { pgt_f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-// largest of three, NaN if one is (a NaN score has to reach its row)
-__device__ __forceinline__ float pgt_max3(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
-
-// 2^x for two x <= 126 on the FMA and integer pipes: x = n + f with n the nearest whole number (adding 1.5 * 2^23
-// leaves it in the low bits) and |f| <= 1/2, 2^f by a polynomial, n added to its exponent.  The coefficients are a
-// minimax fit of 2^f with p(0) = 1 (largest relative error 2.9e-6, far below the rounding of P to bf16).  x is
-// held at -127, where the sum of the exponents is 0: everything below 2^-127, masked scores too, comes out as 0
-// (or less than 2^-126).  The softmax gives some of its exponentials to these pipes because 128 of them per
-// thread and tile keep the SM's MUFU busy for as long as the two products take.
-__device__ __forceinline__ void pgt_exp2_pair(pgt_f2 x, float* e0, float* e1) {
-    float a, b;
-    pgt_unpack(x, &a, &b);
-    x = pgt_pack(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
-    const pgt_f2 r = pgt_add(x, pgt_pack(12582912.0f, 12582912.0f));
-    const pgt_f2 n = pgt_add(r, pgt_pack(-12582912.0f, -12582912.0f));
-    const pgt_f2 f = pgt_fma(n, pgt_pack(-1.0f, -1.0f), x);
-    pgt_f2 p = pgt_fma(f, pgt_pack(0.009582853f, 0.009582853f), pgt_pack(0.055906426f, 0.055906426f));
-    p = pgt_fma(p, f, pgt_pack(0.24024099f, 0.24024099f));
-    p = pgt_fma(p, f, pgt_pack(0.6931242f, 0.6931242f));
-    p = pgt_fma(p, f, pgt_pack(1.0f, 1.0f));
-    float p0, p1, r0, r1;
-    pgt_unpack(p, &p0, &p1);
-    pgt_unpack(r, &r0, &r1);
-    *e0 = __int_as_float(__float_as_int(p0) + (__float_as_int(r0) << 23));
-    *e1 = __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23));
-}
-#ifndef PGT_POLY
-#define PGT_POLY 4                     // of this many pairs of exponentials one goes to the FMA pipe
-#endif
-
 template <int D>
 __global__ void __launch_bounds__(PGT_THREADS, 1)
 pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ PgMaps maps) {
@@ -166,53 +123,36 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
         pg_regs_less<PG_REGS_LESS>();
         if (warp == 8) {
         // ---- producer: K(0) V(0) K(1) V(1) ... of every piece ----
-        const int br = min(1 << p.ge.page_shift, KT), nbox = KT / br;
-        const int no_row = 0x7fffff00;
-        PgWalk walk;
-        walk.start(p, plan);
-        PgPiece pc;
-        int cnt = 0, qn = 0;
-        bool more = true, ok = true, bad = false;
-        while (more && ok) {
-            more = walk.next(p.ge.n_kv, &pc);
-            const int qs = qn % PGT_QUEUE;
-            if (qn >= PGT_QUEUE) ok = mbar_wait(&qu_empty[qs], ((qn / PGT_QUEUE) - 1) & 1);
-            if (!ok) break;
-            if (lane == 0) {
-                if (!more) pc.i1 = -1;
-                queue[qs] = pc;
-                found[qs] = 0;
-                mbar_arrive(&qu_full[qs]);
-            }
-            qn++;
-            if (!more) break;
-            const PgSpan span = pg_span<KT>(pc.pmin, pc.pmax, p.window, p.sinks);
-            for (int i = pc.i0; i < pc.i1 && ok; i++) {
-                const int key = pg_tile_key(span, i, KT) + lane * br;
-                int y = no_row;
-                if (lane < nbox && key <= pc.pmax) {
-                    const long long row = pg_row_of(p.b, p.ge, pc.grp, pc.head, key);
-                    if (row >= 0) y = (int)row;
-                    else if (p.window <= 0 || key < p.sinks || key + br > pc.pmin - p.window + 1) bad = true;
-                }
+        PgProducer<KT, PGT_QUEUE> bx;
+        bx.queue = queue; bx.full = qu_full; bx.empty = qu_empty; bx.found = found;
+        bool ok = bx.start(p, plan);
+        const bool issuer = elect_one();
+        int cnt = 0;
+        while (ok) {
+            const PgPiece* q = bx.begin(p, &ok);
+            if (!q) break;
+            const int i1 = q->i1;
+            for (int i = q->i0; i < i1 && ok; i++) {
+                const int l0 = bx.tile_lane(p, q, i);
                 for (int kv = 0; kv < 2; kv++, cnt++) {
                     const int s = cnt % S;
-                    if (cnt >= S) ok = mbar_wait(&empty[s], ((cnt / S) - 1) & 1);
-                    if (!ok || *abort_flag) { ok = false; break; }
-                    if (lane == 0) mbar_expect_tx(&full[s], C::TILE);
-                    __syncwarp();
-                    if (lane < nbox) {
-                        uint8_t* d = ring + s * C::TILE;
+                    if (cnt >= S && !mbar_wait(&empty[s], ((cnt / S) - 1) & 1)) { ok = false; break; }
+                    uint8_t* d = ring + s * C::TILE;
+                    const CUtensorMap *m64 = kv ? &maps.v64 : &maps.k64, *m32 = kv ? &maps.v32 : &maps.k32;
+                    if (issuer) mbar_expect_tx(&full[s], C::TILE);
+                    for (int b = 0; b < bx.nbox; b++) {
+                        const int y = bx.row(l0 + b), at = b * bx.br;
+                        if (issuer) {
 #pragma unroll
-                        for (int a = 0; a < C::NA; a++)
-                            tma_load_2d(d + a * C::A_BYTES + lane * br * 128, kv ? &maps.v64 : &maps.k64, a * 64, y, &full[s]);
-                        if (C::NB) tma_load_2d(d + C::NA * C::A_BYTES + lane * br * 64, kv ? &maps.v32 : &maps.k32, C::NA * 64, y, &full[s]);
+                            for (int a = 0; a < C::NA; a++) tma_load_2d(d + a * C::A_BYTES + at * 128, m64, a * 64, y, &full[s]);
+                            if (C::NB) tma_load_2d(d + C::NA * C::A_BYTES + at * 64, m32, C::NA * 64, y, &full[s]);
+                        }
                     }
                 }
             }
         }
         if (!ok) *abort_flag = 1;
-        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.w.status, PG_ST_BAD_PAGE);
+        if (__any_sync(0xffffffffu, bx.bad) && lane == 0) atomicOr(p.w.status, PG_ST_BAD_PAGE);
         if (*abort_flag)
             for (int c = max(0, cnt - S); c < cnt; c++) mbar_wait(&full[c % S], (c / S) & 1);
         } else if (warp == 9) {
@@ -370,14 +310,15 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                 uint32_t sr[KT];
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) tmem_ld32_issue(t_s + c, sr + c);
-#pragma unroll
-                for (int c = 0; c < KT; c += 32) tmem_ld32_wait(sr + c);
                 const int key0 = pg_tile_key(span, pc.i0 + j, KT);
                 const bool partial = pg_partial<KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks);
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) tmem_ld32_wait(sr + c);
                 if (partial) {
 #pragma unroll
                     for (int c = 0; c < KT; c += 32) {
                         const uint32_t see = pg_see_bits(key0 + c, pos, lo, p.sinks);
+                        if (__all_sync(0xffffffffu, see == 0xffffffffu)) continue;      // most often a few chunks are cut
 #pragma unroll
                         for (int k = 0; k < 32; k++) sr[c + k] = (see >> k & 1) ? sr[c + k] : 0xff800000u;      // -inf
                     }
