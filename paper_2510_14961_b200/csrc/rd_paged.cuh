@@ -13,7 +13,8 @@
 //
 // Division of the work.  The units of all (row tile, kv head) items - an item's fixed cost, then its key tiles -
 // are numbered in one sequence and cut into one equal contiguous share per block, whatever the batch looks
-// like: one sequence of 131,072 positions is split over all SMs, 64 ragged ones are packed onto them.  An item that lies in one share is
+// like: one sequence of 131,072 positions is split over all SMs, 64 ragged ones are packed onto them.  Items that
+// take less time than joining their parts would are left whole (the block in whose share they begin does them).  An item that lies in one share is
 // finished there; the shares of an item that is cut leave (maximum, sum, unnormalised output) in a workspace,
 // and the block that arrives last joins them in key order, so results do not depend on which block that is.
 #pragma once
@@ -67,6 +68,7 @@ struct PgAttend {
     int inline_plan;             // every block makes the plan itself (few row tiles)
     int min_share;               // units a share has at least
     int item_cost;               // units an item counts for besides its key tiles (its query, its output)
+    int whole_units;             // items of at most this many units are not cut: the block in whose share they begin does them
     int rec_cap;                 // row tiles the plan's array holds (more only come from a group_start that is not ascending)
 };
 
@@ -306,31 +308,34 @@ struct PgPiece {
 // Walks a share piece by piece; every caller that walks (several warps may) sees the same pieces.
 struct PgWalk {
     long long u, u1, per;
-    int rec, head, at, n_rec, cost;
+    int rec, head, at, n_rec, cost, whole;
     const PgRecord* recs;
     template <int CAP> __device__ __forceinline__ void start(const PgAttend& p, const PgPlanSmem<CAP>& sm) {
         u = sm.share.u0; u1 = sm.share.u1; per = sm.share.per;
-        rec = sm.share.rec; head = sm.share.head; at = sm.share.at; n_rec = sm.share.n_rec; cost = p.item_cost;
+        rec = sm.share.rec; head = sm.share.head; at = sm.share.at; n_rec = sm.share.n_rec; cost = p.item_cost; whole = p.whole_units;
         recs = CAP > 1 && p.inline_plan ? sm.rec : p.w.rec;
     }
     __device__ __forceinline__ bool next(int n_kv, PgPiece* o) {
         while (u < u1 && rec < n_rec) {
             const PgRecord r = recs[rec];
             if (r.nt == 0) { rec++; continue; }       // a row tile without a row of a sequence
-            const int units = r.nt + cost, len = (int)min((long long)(units - at), u1 - u);
+            const int units = r.nt + cost;
+            const bool uncut = units <= whole;
+            const int len = uncut ? units - at : (int)min((long long)(units - at), u1 - u);
+            const bool mine = !uncut || at == 0;      // (an uncut item that began in the share before is done there)
             const int i0 = max(0, at - cost), i1 = at + len - cost;
             const long long first = u - at + cost;    // unit of the item's first key tile
             o->grp = r.grp; o->a = r.a; o->n = r.n; o->rt = r.rt; o->head = head;
             o->i0 = i0; o->i1 = i1; o->nt = r.nt; o->pmin = r.pmin; o->pmax = r.pmax;
-            o->c_first = (int)(first / per);
-            o->c_last = (int)((first + r.nt - 1) / per);
+            o->c_first = uncut ? 0 : (int)(first / per);
+            o->c_last = uncut ? 0 : (int)((first + r.nt - 1) / per);
             u += len;
             at += len;
             if (at == units) {
                 at = 0;
                 if (++head == n_kv) { head = 0; rec++; }
             }
-            if (i1 > i0) return true;                 // (a share may end inside an item's fixed cost)
+            if (mine && i1 > i0) return true;                 // (a share may end inside an item's fixed cost)
         }
         return false;
     }

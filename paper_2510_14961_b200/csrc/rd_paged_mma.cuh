@@ -132,71 +132,79 @@ __device__ __forceinline__ void pgt_exp2_pair(pgt_f2 x, float* e0, float* e1) {
 
 // A producer warp's view of a share: it walks the pieces into a queue in shared memory, one ahead of the piece it
 // loads, and turns key tiles into pool rows.  The table is read 32 boxes at a time, one per lane, a chunk ahead of its use
-// (the first chunk of a piece while the piece before it is being loaded), so that no copy waits for a table entry.
+// (the first chunk of a piece while the piece before it is being loaded), and a table entry is not looked at before it
+// is needed, so that no copy waits for one.
 template <int KT, int DEPTH> struct PgProducer {
     PgPiece* queue;                    // [DEPTH]; i1 < 0: no more pieces
-    uint64_t *full, *empty;            // [DEPTH]
+    uint64_t *full, *empty;            // [DEPTH], or null: a queue nobody else reads
     int* found;                        // [DEPTH], cleared with every piece, or null
-    int br, nbox, tpc;                 // positions of a box, boxes of a tile, tiles of a chunk
-    int cur, ahead, first;             // pool rows of this lane's box: current chunk, next chunk, first chunk of the next piece
+    int box_shift, lg_box;             // log2 of a box's positions, of a tile's boxes
+    int cur;                           // pool row of this lane's box of the current chunk
+    int ahead, first;                  // table entries: next chunk, first chunk of the next piece
     int at;                            // lane of the next tile's first box
     int qn;                            // pieces pushed
     bool bad;
     PgWalk walk;
-    __device__ __forceinline__ int look(const PgAttend& p, const PgPiece& q, int i_first) {
-        const int lane = threadIdx.x & 31, i = i_first + lane / nbox;
-        int y = 0x7fffff00;            // beyond the pages: the box reads as zeros
-        if (i < q.i1) {
-            const int key = pg_tile_key(pg_span<KT>(q.pmin, q.pmax, p.window, p.sinks), i, KT) + (lane % nbox) * br;
-            if (key <= q.pmax) {
-                const long long row = pg_row_of(p.b, p.ge, q.grp, q.head, key);
-                if (row >= 0) y = (int)row;
-                else if (p.window <= 0 || key < p.sinks || key + br > q.pmin - p.window + 1) bad = true;      // a page some row needs
-            }
-        }
-        return y;
+    __device__ __forceinline__ int key_of(const PgAttend& p, const PgPiece& q, int i) const {      // of this lane's box, -1: none
+        const int lane = threadIdx.x & 31;
+        i += lane >> lg_box;
+        if (i >= q.i1) return -1;
+        const int key = pg_tile_key(pg_span<KT>(q.pmin, q.pmax, p.window, p.sinks), i, KT) + ((lane & ((1 << lg_box) - 1)) << box_shift);
+        return key <= q.pmax ? key : -1;
     }
-    // the next piece (or the end) into the queue, and the rows of its first boxes; false: a wait ran out
+    __device__ __forceinline__ int entry(const PgAttend& p, const PgPiece& q, int i) const {
+        const int key = key_of(p, q, i), pi = key >> p.ge.page_shift;
+        return key >= 0 && pi < p.b.table_stride ? p.b.table[(size_t)q.grp * p.b.table_stride + pi] : -1;
+    }
+    __device__ __forceinline__ int resolve(const PgAttend& p, const PgPiece& q, int i, int pg) {
+        const int key = key_of(p, q, i);
+        if (key < 0) return 0x7fffff00;            // beyond the pages: the box reads as zeros
+        if (pg < 0 || pg >= p.ge.n_pages) {
+            if (p.window <= 0 || key < p.sinks || key + (1 << box_shift) > q.pmin - p.window + 1) bad = true;      // a page some row needs
+            return 0x7fffff00;
+        }
+        return ((((p.ge.layer * p.ge.n_pages + pg) * p.ge.n_kv) + q.head) << p.ge.page_shift) + (key & ((1 << p.ge.page_shift) - 1));
+    }
+    // the next piece (or the end) into the queue, the table entries of its first boxes on their way; false: a wait ran out
     __device__ __forceinline__ bool push(const PgAttend& p) {
         PgPiece pc;
         const bool more = walk.next(p.ge.n_kv, &pc);
         const int s = qn % DEPTH;
-        if (qn >= DEPTH && !mbar_wait(&empty[s], ((qn / DEPTH) - 1) & 1)) return false;
+        if (empty && qn >= DEPTH && !mbar_wait(&empty[s], ((qn / DEPTH) - 1) & 1)) return false;
         if ((threadIdx.x & 31) == 0) {
             if (!more) pc.i1 = -1;
             queue[s] = pc;
             if (found) found[s] = 0;
-            mbar_arrive(&full[s]);
+            if (full) mbar_arrive(&full[s]);
         }
         __syncwarp();
         qn++;
-        if (more) first = look(p, queue[s], queue[s].i0);
+        if (more) first = entry(p, queue[s], queue[s].i0);
         return true;
     }
     template <typename Plan> __device__ __forceinline__ bool start(const PgAttend& p, const Plan& plan) {
-        br = min(1 << p.ge.page_shift, KT);
-        nbox = KT / br;
-        tpc = 32 / nbox;
+        box_shift = min(p.ge.page_shift, KT == 32 ? 5 : 7);
+        static_assert(KT == 32 || KT == 128, "tile heights of the two kernels");
+        lg_box = (KT == 32 ? 5 : 7) - box_shift;
         bad = false;
         qn = 0;
         walk.start(p, plan);
         return push(p);
     }
-    // begins the oldest piece that has not been loaded (null: none is left, or a wait ran out: *ok)
-    __device__ __forceinline__ const PgPiece* begin(const PgAttend& p, bool* ok) {
+    // begins the piece pushed last (null: the end); push() the next one once the first tile has been asked for
+    __device__ __forceinline__ const PgPiece* begin(const PgAttend& p) {
         const PgPiece* q = &queue[(qn - 1) % DEPTH];
         if (q->i1 < 0) return nullptr;
-        cur = first;
+        cur = resolve(p, *q, q->i0, first);
+        ahead = entry(p, *q, q->i0 + (32 >> lg_box));
         at = 0;
-        ahead = look(p, *q, q->i0 + tpc);
-        *ok = push(p);
-        return *ok ? q : nullptr;
+        return q;
     }
     // lane that holds the row of tile i's first box; tiles are asked for in order, from the piece's first
     __device__ __forceinline__ int tile_lane(const PgAttend& p, const PgPiece* q, int i) {
-        if (at == 32) { cur = ahead; ahead = look(p, *q, i + tpc); at = 0; }
+        if (at == 32) { cur = resolve(p, *q, i, ahead); ahead = entry(p, *q, i + (32 >> lg_box)); at = 0; }
         const int l = at;
-        at += nbox;
+        at += 1 << lg_box;
         return l;
     }
     __device__ __forceinline__ int row(int lane) const { return __shfl_sync(0xffffffffu, cur, lane); }
@@ -214,7 +222,7 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
     float* MLs = reinterpret_cast<float*>(ring + C::RING + C::O_BYTES);
     __shared__ PgPlanSmem<PG_INLINE_REC> plan;
     __shared__ uint64_t full[S], empty[S], q_full[PGM_QUEUE], q_empty[PGM_QUEUE];
-    __shared__ PgPiece queue[PGM_QUEUE];          // i1 < 0: no more pieces
+    __shared__ PgPiece queue[PGM_QUEUE], queue_v[PGM_QUEUE];          // i1 < 0: no more pieces
     __shared__ int abort_s, stop_s, flag_s, found_s;
     volatile int* abort_flag = &abort_s;
 
@@ -222,7 +230,7 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
     if (tid == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k64) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.v64) : "memory");
-        for (int s = 0; s < S; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], WQ); }
+        for (int s = 0; s < S; s++) { mbar_init(&full[s], 2); mbar_init(&empty[s], WQ); }
         for (int s = 0; s < PGM_QUEUE; s++) { mbar_init(&q_full[s], 1); mbar_init(&q_empty[s], 1); }
         abort_s = 0; stop_s = 0; found_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -233,38 +241,36 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
 
     if (warp >= 8) {
         pg_regs_less<PG_REGS_LESS>();
-        if (warp == 8) {
-        // ---- producer ----
+        if (warp <= 9) {
+        // ---- producers: warp 8 the K tiles (and the queue of pieces), warp 9 the V tiles ----
+        const bool is_v = warp == 9;
         PgProducer<PGM_KT, PGM_QUEUE> bx;
-        bx.queue = queue; bx.full = q_full; bx.empty = q_empty; bx.found = nullptr;
+        bx.queue = is_v ? queue_v : queue; bx.full = is_v ? nullptr : q_full; bx.empty = is_v ? nullptr : q_empty; bx.found = nullptr;
         bool ok = bx.start(p, plan);
         const bool issuer = elect_one();
+        const CUtensorMap *m64 = is_v ? &maps.v64 : &maps.k64, *m32 = is_v ? &maps.v32 : &maps.k32;
+        uint8_t* const base = ring + (is_v ? T::BYTES : 0);
+        const int nbox = 1 << bx.lg_box;
         int cnt = 0;
         while (ok) {
-            const PgPiece* q = bx.begin(p, &ok);
+            const PgPiece* q = bx.begin(p);
             if (!q) break;
-            const int i1 = q->i1;
-            for (int i = q->i0; i < i1; i++, cnt++) {
+            const int i0 = q->i0, i1 = q->i1;
+            for (int i = i0; i < i1; i++, cnt++) {
                 const int s = cnt % S, l0 = bx.tile_lane(p, q, i);
                 if (cnt >= S && !mbar_wait(&empty[s], ((cnt / S) - 1) & 1)) { ok = false; break; }
-                uint8_t* kd = ring + s * C::STAGE_BYTES;
-                uint8_t* vd = kd + T::BYTES;
-                if (issuer) mbar_expect_tx(&full[s], C::STAGE_BYTES);
+                uint8_t* dst = base + s * C::STAGE_BYTES;
+                if (issuer) mbar_expect_tx(&full[s], T::BYTES);
 #pragma unroll 1
-                for (int b = 0; b < bx.nbox; b++) {
-                    const int y = bx.row(l0 + b), at = b * bx.br;
+                for (int b = 0; b < nbox; b++) {
+                    const int y = bx.row(l0 + b), at = b << bx.box_shift;
                     if (issuer) {
 #pragma unroll
-                        for (int a = 0; a < T::NA; a++) {
-                            tma_load_2d(kd + a * T::A_BYTES + at * 128, &maps.k64, a * 64, y, &full[s]);
-                            tma_load_2d(vd + a * T::A_BYTES + at * 128, &maps.v64, a * 64, y, &full[s]);
-                        }
-                        if (T::NB) {
-                            tma_load_2d(kd + T::NA * T::A_BYTES + at * 64, &maps.k32, T::NA * 64, y, &full[s]);
-                            tma_load_2d(vd + T::NA * T::A_BYTES + at * 64, &maps.v32, T::NA * 64, y, &full[s]);
-                        }
+                        for (int a = 0; a < T::NA; a++) tma_load_2d(dst + a * T::A_BYTES + at * 128, m64, a * 64, y, &full[s]);
+                        if (T::NB) tma_load_2d(dst + T::NA * T::A_BYTES + at * 64, m32, T::NA * 64, y, &full[s]);
                     }
                 }
+                if (i == i0 && !bx.push(p)) { cnt++; ok = false; break; }
             }
         }
         if (!ok) *abort_flag = 1;

@@ -7,8 +7,9 @@
 // A's softmax under B's products and the other way round.
 //   warps 0-3 / 4-7  softmax of A / B: one packed row per thread (TMEM lane = row); S from TMEM to registers, mask,
 //                    online softmax in float32, P (bf16) back into the columns S came from
-//   warp 8           walks the block's share (rd_paged.cuh) and fills a ring of K and V tiles by TMA, one box per
-//                    page piece; it runs ahead across items
+//   warps 8, 10      walk the block's share (rd_paged.cuh) and fill a ring of K and V tiles by TMA, one box per page
+//                    piece; they run ahead across items
+//   warp 11          looks through the V tiles of which some row does not see every key (see below)
 //   warp 9           issues the MMAs: S_A(0) S_B(0), then PV_A(j) S_A(j+1) PV_B(j) S_B(j+1); P is the A operand
 //                    from TMEM, V the MN-major B operand as it lies in its page
 // TMEM: S/P of A and B (128 columns each), O of A and B (D columns each).  MMAs complete in the order they are
@@ -95,9 +96,9 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
     uint8_t* Qs = (uint8_t*)(((uintptr_t)pgt_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* ring = Qs + 2 * C::TILE;
     __shared__ PgPlanSmem<1> plan;
-    __shared__ uint64_t full[S], empty[S], qu_full[PGT_QUEUE], qu_empty[PGT_QUEUE];
+    __shared__ uint64_t full[S], empty[S], clean[S], qu_full[PGT_QUEUE], qu_empty[PGT_QUEUE];
     __shared__ uint64_t q_full[2], s_full[2], p_lo[2], p_hi[2], o_full[2];     // P in two parts: 96 keys, 32 keys
-    __shared__ PgPiece queue[PGT_QUEUE];
+    __shared__ PgPiece queue[PGT_QUEUE], queue_v[PGT_QUEUE];
     __shared__ int found[PGT_QUEUE];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_s;
@@ -105,8 +106,8 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int s = 0; s < S; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int s = 0; s < PGT_QUEUE; s++) { mbar_init(&qu_full[s], 1); mbar_init(&qu_empty[s], 9); }
+        for (int s = 0; s < S; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); mbar_init(&clean[s], 1); }
+        for (int s = 0; s < PGT_QUEUE; s++) { mbar_init(&qu_full[s], 1); mbar_init(&qu_empty[s], 10); }
         for (int w = 0; w < 2; w++) { mbar_init(&q_full[w], 4); mbar_init(&s_full[w], 1); mbar_init(&p_lo[w], 4); mbar_init(&p_hi[w], 4); mbar_init(&o_full[w], 1); }
         abort_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -121,40 +122,84 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
 
     if (warp >= 8) {
         pg_regs_less<PG_REGS_LESS>();
-        if (warp == 8) {
-        // ---- producer: K(0) V(0) K(1) V(1) ... of every piece ----
+        if (warp == 8 || warp == 10) {
+        // ---- producers: K(0) V(0) K(1) V(1) ... of every piece, warp 8 the K tiles (and the queue), warp 10 the V tiles ----
+        const int kv = warp == 10;
         PgProducer<KT, PGT_QUEUE> bx;
-        bx.queue = queue; bx.full = qu_full; bx.empty = qu_empty; bx.found = found;
+        bx.queue = kv ? queue_v : queue; bx.full = kv ? nullptr : qu_full; bx.empty = kv ? nullptr : qu_empty; bx.found = kv ? nullptr : found;
         bool ok = bx.start(p, plan);
         const bool issuer = elect_one();
-        int cnt = 0;
+        const CUtensorMap *m64 = kv ? &maps.v64 : &maps.k64, *m32 = kv ? &maps.v32 : &maps.k32;
+        const int nbox = 1 << bx.lg_box;
+        int cnt = kv;
         while (ok) {
-            const PgPiece* q = bx.begin(p, &ok);
+            const PgPiece* q = bx.begin(p);
             if (!q) break;
-            const int i1 = q->i1;
-            for (int i = q->i0; i < i1 && ok; i++) {
-                const int l0 = bx.tile_lane(p, q, i);
-                for (int kv = 0; kv < 2; kv++, cnt++) {
-                    const int s = cnt % S;
-                    if (cnt >= S && !mbar_wait(&empty[s], ((cnt / S) - 1) & 1)) { ok = false; break; }
-                    uint8_t* d = ring + s * C::TILE;
-                    const CUtensorMap *m64 = kv ? &maps.v64 : &maps.k64, *m32 = kv ? &maps.v32 : &maps.k32;
-                    if (issuer) mbar_expect_tx(&full[s], C::TILE);
-                    for (int b = 0; b < bx.nbox; b++) {
-                        const int y = bx.row(l0 + b), at = b * bx.br;
-                        if (issuer) {
+            const int i0 = q->i0, i1 = q->i1;
+            for (int i = i0; i < i1; i++, cnt += 2) {
+                const int s = cnt % S, l0 = bx.tile_lane(p, q, i);
+                if (cnt >= S && !mbar_wait(&empty[s], ((cnt / S) - 1) & 1)) { ok = false; break; }
+                uint8_t* d = ring + s * C::TILE;
+                if (issuer) mbar_expect_tx(&full[s], C::TILE);
+#pragma unroll 1
+                for (int b = 0; b < nbox; b++) {
+                    const int y = bx.row(l0 + b), at = b << bx.box_shift;
+                    if (issuer) {
 #pragma unroll
-                            for (int a = 0; a < C::NA; a++) tma_load_2d(d + a * C::A_BYTES + at * 128, m64, a * 64, y, &full[s]);
-                            if (C::NB) tma_load_2d(d + C::NA * C::A_BYTES + at * 64, m32, C::NA * 64, y, &full[s]);
-                        }
+                        for (int a = 0; a < C::NA; a++) tma_load_2d(d + a * C::A_BYTES + at * 128, m64, a * 64, y, &full[s]);
+                        if (C::NB) tma_load_2d(d + C::NA * C::A_BYTES + at * 64, m32, C::NA * 64, y, &full[s]);
                     }
                 }
+                if (i == i0 && !bx.push(p)) { cnt += 2; ok = false; break; }
             }
         }
         if (!ok) *abort_flag = 1;
         if (__any_sync(0xffffffffu, bx.bad) && lane == 0) atomicOr(p.w.status, PG_ST_BAD_PAGE);
         if (*abort_flag)
-            for (int c = max(0, cnt - S); c < cnt; c++) mbar_wait(&full[c % S], (c / S) & 1);
+            for (int c = cnt - 2; c >= max(0, cnt - S); c -= 2) mbar_wait(&full[c % S], (c / S) & 1);
+        } else if (warp == 11) {
+        // ---- V tiles that some row does not see all of: non-finite elements out, before anyone multiplies by them ----
+        int cnt = 1;
+        bool ok = true;
+        for (int qn = 0; ok; qn++) {
+            const int qs = qn % PGT_QUEUE;
+            ok = !*abort_flag && mbar_wait(&qu_full[qs], (qn / PGT_QUEUE) & 1);
+            if (!ok) break;
+            const PgPiece pc = queue[qs];
+            if (pc.i1 < 0) break;
+            const PgSpan span = pg_span<KT>(pc.pmin, pc.pmax, p.window, p.sinks);
+            for (int i = pc.i0; i < pc.i1 && ok; i++, cnt += 2) {
+                const int s = cnt % S;
+                ok = mbar_wait(&full[s], (cnt / S) & 1);
+                if (ok && pg_partial<KT>(pg_tile_key(span, i, KT), pc.pmin, pc.pmax, p.window, p.sinks)) {
+                    uint8_t* vt = ring + s * C::TILE;
+                    // 16-byte chunks in the order they lie in: D * 128 / 8 of them, the same for every swizzle
+                    uint32_t seen = 0;
+#pragma unroll 8
+                    for (int c = lane; c < C::TILE / 16; c += 32) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(vt + c * 16);      // an exponent of all ones carries into bit 15 (31)
+                        seen |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) |
+                                ((v.z & 0x7f807f80u) + 0x00800080u) | ((v.w & 0x7f807f80u) + 0x00800080u);
+                    }
+                    if (seen & 0x80008000u) {
+                        bool hit;
+                        for (int c = lane; c < C::TILE / 16; c += 32) {
+                            uint4 v = *reinterpret_cast<const uint4*>(vt + c * 16);
+                            v.x = pgm_finite(v.x, &hit); v.y = pgm_finite(v.y, &hit); v.z = pgm_finite(v.z, &hit); v.w = pgm_finite(v.w, &hit);
+                            *reinterpret_cast<uint4*>(vt + c * 16) = v;
+                        }
+                        *(volatile int*)&found[qs] = 1;
+                        __threadfence_block();
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive(&clean[s]);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&qu_empty[qs]);
+        }
+        if (!ok) *abort_flag = 1;
         } else if (warp == 9) {
         // ---- MMA issuer ----
         constexpr uint32_t idesc_s = umma_idesc(KT);
@@ -200,6 +245,8 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                         umma_bf16_ts(d + C::NA * 64, a0 + k * 8, umma_desc_mn64(v0 + C::NA * C::A_BYTES + k * 1024), idesc_o32, (!first || k) ? 1u : 0u);
                 }
             };
+            // uses of a stage by V tiles before load c: every use where K and V keep to their stages (S even), every other one else
+            auto v_phase = [](int c) { return (uint32_t)(S % 2 ? (c / S) >> 1 : c / S) & 1u; };
             const bool issuer = elect_one();
             ok = mbar_wait(&full[cnt % S], (cnt / S) & 1);
             for (int w = 0; w < nb && ok; w++) {
@@ -213,7 +260,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
             for (int j = 0; j < len && ok; j++) {
                 const int cv = cnt + 2 * j + 1, ck = cv + 1;
                 const bool more = j + 1 < len;
-                ok = mbar_wait(&full[cv % S], (cv / S) & 1) && (!more || mbar_wait(&full[ck % S], (ck / S) & 1));
+                ok = mbar_wait(&clean[cv % S], v_phase(cv)) && (!more || mbar_wait(&full[ck % S], (ck / S) & 1));
                 for (int w = 0; w < nb && ok; w++) {
                     ok = !*abort_flag && mbar_wait(&p_lo[w], np[w] & 1);
                     if (ok && issuer) pv(w, cv, j == 0, 0, 6);
@@ -251,7 +298,6 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
         const int limit = pg_pos_limit(p.b, p.ge);
         const float c2 = p.scale_log2;
         uint32_t n_s = 0, n_o = 0;
-        int cnt = 0;
         bool ok = true;
         for (int qn = 0; ok; qn++) {
             const int qs = qn % PGT_QUEUE;
@@ -269,7 +315,6 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
             int pos = have ? p.b.row_pos[row] : -1;
             if (pos >= limit) pos = -1;
             if (w == 1 && packed - (unsigned)pc.rt * M <= 128u) {             // block B is empty
-                cnt += 2 * len;
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(&q_full[1]); mbar_arrive(&qu_empty[qs]); }
                 continue;
@@ -347,35 +392,6 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                 }
                 if (move) m = mx;
                 const float u = m == -INFINITY ? 0.f : m;
-                if (partial && w == 0) {
-                    // thread = key: take non-finite elements out of this V tile before anyone multiplies by it
-                    const int cv = cnt + 2 * j + 1;
-                    ok = __all_sync(0xffffffffu, mbar_wait(&full[cv % S], (cv / S) & 1));
-                    if (!ok) break;
-                    uint8_t* vt = ring + (cv % S) * C::TILE;
-auto at = [&](int c) {
-                        return reinterpret_cast<uint4*>(c < 8 * C::NA ? vt + (c >> 3) * C::A_BYTES + rl * 128 + (((c & 7) ^ (rl & 7)) << 4)
-                                                                      : vt + C::NA * C::A_BYTES + rl * 64 + (((c & 3) ^ ((rl >> 1) & 3)) << 4));
-                    };
-                    uint32_t seen = 0;
-#pragma unroll
-                    for (int c = 0; c < D / 8; c++) {
-                        const uint4 v = *at(c);        // an exponent of all ones carries into bit 15 (31)
-                        seen |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) |
-                                ((v.z & 0x7f807f80u) + 0x00800080u) | ((v.w & 0x7f807f80u) + 0x00800080u);
-                    }
-                    bool hit = (seen & 0x80008000u) != 0;
-                    if (hit) {
-#pragma unroll 1
-                        for (int c = 0; c < D / 8; c++) {
-                            uint4 v = *at(c);
-                            v.x = pgm_finite(v.x, &hit); v.y = pgm_finite(v.y, &hit); v.z = pgm_finite(v.z, &hit); v.w = pgm_finite(v.w, &hit);
-                            *at(c) = v;
-                        }
-                    }
-                    if (hit) { *(volatile int*)&found[qs] = 1; __threadfence_block(); }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
                 const pgt_f2 cc = pgt_pack(c2, c2), uu = pgt_pack(-u, -u);
                 pgt_f2 sums[2] = {0ull, 0ull};
                 // P of 32 keys (16 packed words) from their scores
@@ -418,7 +434,6 @@ auto at = [&](int c) {
             }
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&o_full[w], n_o & 1));
             n_o++;
-            cnt += 2 * len;
             if (!ok) { *abort_flag = 1; break; }
             tc_fence_after();
             const bool whole = pc.c_first == pc.c_last, fix = *(volatile int*)&found[qs] != 0;
