@@ -70,7 +70,7 @@ __device__ __forceinline__ uint32_t pgm_finite(uint32_t x, bool* found) {
 // key tiles [i0, i1) that were multiplied without them (partial tiles).  A weight is positive, so an infinity
 // stays one.  Rare, hence slow and simple.
 template <int KT>
-__device__ float pg_nonfinite(const PgAttend& p, const PgPiece& pc, int pos, int e) {
+__device__ __noinline__ float pg_nonfinite(const PgAttend& p, const PgPiece& pc, int pos, int e) {
     const PgSpan span = pg_span<KT>(pc.pmin, pc.pmax, p.window, p.sinks);
     float add = 0.f;
     for (int i = pc.i0; i < pc.i1; i++) {
@@ -93,42 +93,6 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
     return yes != 0;
 }
-
-// Two floats at once (the FMA pipe's packed forms).
-typedef unsigned long long pgt_f2;
-__device__ __forceinline__ pgt_f2 pgt_pack(float a, float b) { pgt_f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void pgt_unpack(pgt_f2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
-__device__ __forceinline__ pgt_f2 pgt_fma(pgt_f2 a, pgt_f2 b, pgt_f2 c) { pgt_f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ pgt_f2 pgt_add(pgt_f2 a, pgt_f2 b) { pgt_f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-// largest of three, NaN if one is (a NaN score has to reach its row)
-__device__ __forceinline__ float pgt_max3(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
-
-// 2^x for two x <= 126 on the FMA and integer pipes: x = n + f with n the nearest whole number (adding 1.5 * 2^23
-// leaves it in the low bits) and |f| <= 1/2, 2^f by a polynomial, n added to its exponent.  The coefficients are a
-// minimax fit of 2^f with p(0) = 1 (largest relative error 2.9e-6, far below the rounding of P to bf16).  x is
-// held at -127, where the sum of the exponents is 0: everything below 2^-127, masked scores too, comes out as 0
-// (or less than 2^-126).  The softmax gives some of its exponentials to these pipes because 128 of them per
-// thread and tile keep the SM's MUFU busy for as long as the two products take.
-__device__ __forceinline__ void pgt_exp2_pair(pgt_f2 x, float* e0, float* e1) {
-    float a, b;
-    pgt_unpack(x, &a, &b);
-    x = pgt_pack(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
-    const pgt_f2 r = pgt_add(x, pgt_pack(12582912.0f, 12582912.0f));
-    const pgt_f2 n = pgt_add(r, pgt_pack(-12582912.0f, -12582912.0f));
-    const pgt_f2 f = pgt_fma(n, pgt_pack(-1.0f, -1.0f), x);
-    pgt_f2 p = pgt_fma(f, pgt_pack(0.009582853f, 0.009582853f), pgt_pack(0.055906426f, 0.055906426f));
-    p = pgt_fma(p, f, pgt_pack(0.24024099f, 0.24024099f));
-    p = pgt_fma(p, f, pgt_pack(0.6931242f, 0.6931242f));
-    p = pgt_fma(p, f, pgt_pack(1.0f, 1.0f));
-    float p0, p1, r0, r1;
-    pgt_unpack(p, &p0, &p1);
-    pgt_unpack(r, &r0, &r1);
-    *e0 = __int_as_float(__float_as_int(p0) + (__float_as_int(r0) << 23));
-    *e1 = __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23));
-}
-#ifndef PGT_POLY
-#define PGT_POLY 4                     // of this many pairs of exponentials one goes to the FMA pipe
-#endif
 
 // A producer warp's view of a share: it walks the pieces into a queue in shared memory, one ahead of the piece it
 // loads, and turns key tiles into pool rows.  The table is read 32 boxes at a time, one per lane, a chunk ahead of its use

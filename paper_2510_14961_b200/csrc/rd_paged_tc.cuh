@@ -87,6 +87,42 @@ __device__ __forceinline__ uint64_t umma_desc_mn128_blocks(uint32_t saddr, uint3
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(apart >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
+// Two floats at once (the FMA pipe's packed forms).
+typedef unsigned long long pgt_f2;
+__device__ __forceinline__ pgt_f2 pgt_pack(float a, float b) { pgt_f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void pgt_unpack(pgt_f2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
+__device__ __forceinline__ pgt_f2 pgt_fma(pgt_f2 a, pgt_f2 b, pgt_f2 c) { pgt_f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ pgt_f2 pgt_add(pgt_f2 a, pgt_f2 b) { pgt_f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+// largest of three, NaN if one is (a NaN score has to reach its row)
+__device__ __forceinline__ float pgt_max3(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+
+// 2^x for two x <= 126 on the FMA and integer pipes: x = n + f with n the nearest whole number (adding 1.5 * 2^23
+// leaves it in the low bits) and |f| <= 1/2, 2^f by a polynomial, n added to its exponent.  The coefficients are a
+// minimax fit of 2^f with p(0) = 1 (largest relative error 2.9e-6, far below the rounding of P to bf16).  x is
+// held at -127, where the sum of the exponents is 0: everything below 2^-127, masked scores too, comes out as 0
+// (or less than 2^-126).  The softmax gives some of its exponentials to these pipes because 128 of them per
+// thread and tile keep the SM's MUFU busy for as long as the two products take.
+__device__ __forceinline__ void pgt_exp2_pair(pgt_f2 x, float* e0, float* e1) {
+    float a, b;
+    pgt_unpack(x, &a, &b);
+    x = pgt_pack(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
+    const pgt_f2 r = pgt_add(x, pgt_pack(12582912.0f, 12582912.0f));
+    const pgt_f2 n = pgt_add(r, pgt_pack(-12582912.0f, -12582912.0f));
+    const pgt_f2 f = pgt_fma(n, pgt_pack(-1.0f, -1.0f), x);
+    pgt_f2 p = pgt_fma(f, pgt_pack(0.009582853f, 0.009582853f), pgt_pack(0.055906426f, 0.055906426f));
+    p = pgt_fma(p, f, pgt_pack(0.24024099f, 0.24024099f));
+    p = pgt_fma(p, f, pgt_pack(0.6931242f, 0.6931242f));
+    p = pgt_fma(p, f, pgt_pack(1.0f, 1.0f));
+    float p0, p1, r0, r1;
+    pgt_unpack(p, &p0, &p1);
+    pgt_unpack(r, &r0, &r1);
+    *e0 = __int_as_float(__float_as_int(p0) + (__float_as_int(r0) << 23));
+    *e1 = __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23));
+}
+#ifndef PGT_POLY
+#define PGT_POLY 4                     // of this many pairs of exponentials one goes to the FMA pipe
+#endif
+
 template <int D>
 __global__ void __launch_bounds__(PGT_THREADS, 1)
 pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ PgMaps maps) {
@@ -352,55 +388,34 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                 if (!ok) break;
                 n_s++;
                 tc_fence_after();
-                uint32_t sr[KT];
-#pragma unroll
-                for (int c = 0; c < KT; c += 32) tmem_ld32_issue(t_s + c, sr + c);
                 const int key0 = pg_tile_key(span, pc.i0 + j, KT);
-                const bool partial = pg_partial<KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks);
-#pragma unroll
-                for (int c = 0; c < KT; c += 32) tmem_ld32_wait(sr + c);
-                if (partial) {
-#pragma unroll
-                    for (int c = 0; c < KT; c += 32) {
-                        const uint32_t see = pg_see_bits(key0 + c, pos, lo, p.sinks);
-                        if (__all_sync(0xffffffffu, see == 0xffffffffu)) continue;      // most often a few chunks are cut
-#pragma unroll
-                        for (int k = 0; k < 32; k++) sr[c + k] = (see >> k & 1) ? sr[c + k] : 0xff800000u;      // -inf
-                    }
-                }
-                float mx4[4] = {__uint_as_float(sr[0]), __uint_as_float(sr[1]), __uint_as_float(sr[2]), __uint_as_float(sr[3])};
-#pragma unroll
-                for (int k = 4; k + 8 <= KT; k += 8)
-#pragma unroll
-                    for (int q = 0; q < 4; q++) mx4[q] = pgt_max3(mx4[q], __uint_as_float(sr[k + 2 * q]), __uint_as_float(sr[k + 2 * q + 1]));
-                mx4[0] = pgt_max3(mx4[0], __uint_as_float(sr[KT - 4]), __uint_as_float(sr[KT - 3]));
-                mx4[1] = pgt_max3(mx4[1], __uint_as_float(sr[KT - 2]), __uint_as_float(sr[KT - 1]));
-                const float mx = pgt_max3(pgt_max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]) * c2;
-                const bool move = !(mx <= m + 8.0f) || (m == -INFINITY && mx > -INFINITY);      // (a NaN moves it, too)
-                if (__any_sync(0xffffffffu, move && l > 0.f)) {
-                    // O is at rest: the commit that announced S(j) covers P V(j - 1)
-                    const float corr = move ? ex2_approx(m - mx) : 1.0f;
-#pragma unroll
-                    for (int c = 0; c < D; c += 32) {
-                        uint32_t orow[32];
-                        tmem_ld32(t_o + c, orow);
-#pragma unroll
-                        for (int k = 0; k < 32; k++) orow[k] = __float_as_uint(__uint_as_float(orow[k]) * corr);
-                        tmem_st32(t_o + c, orow);
-                    }
-                    l *= corr;
-                }
-                if (move) m = mx;
-                const float u = m == -INFINITY ? 0.f : m;
-                const pgt_f2 cc = pgt_pack(c2, c2), uu = pgt_pack(-u, -u);
                 pgt_f2 sums[2] = {0ull, 0ull};
-                // P of 32 keys (16 packed words) from their scores
-                auto exps = [&](const uint32_t* s, uint32_t* pw) {
+                // moves the row's maximum to `mx` where the tile asks for it, and O and l with it
+                auto settle = [&](float mx) {
+                    const bool move = !(mx <= m + 8.0f) || (m == -INFINITY && mx > -INFINITY);      // (a NaN moves it, too)
+                    if (__any_sync(0xffffffffu, move && l > 0.f)) {
+                        // O is at rest: the commit that announced S(j) covers P V(j - 1)
+                        const float corr = move ? ex2_approx(m - mx) : 1.0f;
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t orow[32];
+                            tmem_ld32(t_o + c, orow);
+#pragma unroll
+                            for (int k = 0; k < 32; k++) orow[k] = __float_as_uint(__uint_as_float(orow[k]) * corr);
+                            tmem_st32(t_o + c, orow);
+                        }
+                        l *= corr;
+                    }
+                    if (move) m = mx;
+                };
+                const pgt_f2 cc = pgt_pack(c2, c2);
+                // P of 32 keys (16 packed words) from their scores, one pair of every `poly` on the FMA pipe
+                auto exps = [&](const uint32_t* s, uint32_t* pw, pgt_f2 uu, int poly) {
 #pragma unroll
                     for (int k = 0; k < 16; k++) {
                         const pgt_f2 x = pgt_fma(pgt_pack(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), cc, uu);
                         float e0, e1;
-                        if (k % PGT_POLY == PGT_POLY - 1) {
+                        if (k % poly == poly - 1) {
                             pgt_exp2_pair(x, &e0, &e1);
                         } else {
                             pgt_unpack(x, &e0, &e1);
@@ -411,18 +426,73 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                         pw[k] = pack_bf16(e0, e1);
                     }
                 };
-                uint32_t pw[32];
-                exps(sr, pw);
-                exps(sr + 32, pw + 16);
-                tmem_st32_issue(t_s, pw);
-                exps(sr + 64, pw);
-                tmem_st16_issue(t_s + 32, pw);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_lo[w]);      // the product may begin with these 96 keys
-                exps(sr + 96, pw);
-                tmem_st16_issue(t_s + 48, pw);
+                auto max32 = [&](const uint32_t* s, float* mx4) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8)
+#pragma unroll
+                        for (int q = 0; q < 4; q++) mx4[q] = pgt_max3(mx4[q], __uint_as_float(s[k + 2 * q]), __uint_as_float(s[k + 2 * q + 1]));
+                };
+                float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                if (!pg_partial<KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks)) {
+                    // every row sees every key: the whole row of S in registers, read once
+                    uint32_t sr[KT], pw[32];
+#pragma unroll
+                    for (int c = 0; c < KT; c += 32) tmem_ld32_issue(t_s + c, sr + c);
+#pragma unroll
+                    for (int c = 0; c < KT; c += 32) tmem_ld32_wait(sr + c);
+#pragma unroll
+                    for (int c = 0; c < KT; c += 32) max32(sr + c, mx4);
+                    settle(pgt_max3(pgt_max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]) * c2);
+                    const float u = m == -INFINITY ? 0.f : m;
+                    const pgt_f2 uu = pgt_pack(-u, -u);
+                    exps(sr, pw, uu, PGT_POLY);
+                    exps(sr + 32, pw + 16, uu, PGT_POLY);
+                    tmem_st32_issue(t_s, pw);
+                    exps(sr + 64, pw, uu, PGT_POLY);
+                    tmem_st16_issue(t_s + 32, pw);
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_lo[w]);      // the product may begin with these 96 keys
+                    exps(sr + 96, pw, uu, PGT_POLY);
+                    tmem_st16_issue(t_s + 48, pw);
+                } else {
+                    // a tile with masked keys: 32 keys at a time in loops that stay small (unrolled like the path above, the
+                    // masks cost more in instruction fetches than in work), S read twice; P goes where S has been read
+                    uint32_t sr[32], pw[16];
+#pragma unroll 1
+                    for (int c = 0; c < KT; c += 32) {
+                        const uint32_t see = pg_see_bits(key0 + c, pos, lo, p.sinks);
+                        if (!__any_sync(0xffffffffu, see != 0)) continue;
+                        tmem_ld32(t_s + c, sr);
+#pragma unroll
+                        for (int k = 0; k < 32; k++) sr[k] = (see >> k & 1) ? sr[k] : 0xff800000u;      // -inf
+                        max32(sr, mx4);
+                    }
+                    settle(pgt_max3(pgt_max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]) * c2);
+                    const float u = m == -INFINITY ? 0.f : m;
+                    const pgt_f2 uu = pgt_pack(-u, -u);
+#pragma unroll 1
+                    for (int c = 0; c < KT; c += 32) {
+                        const uint32_t see = pg_see_bits(key0 + c, pos, lo, p.sinks);
+                        if (__any_sync(0xffffffffu, see != 0)) {
+                            tmem_ld32(t_s + c, sr);
+#pragma unroll
+                            for (int k = 0; k < 32; k++) sr[k] = (see >> k & 1) ? sr[k] : 0xff800000u;
+                            exps(sr, pw, uu, PGT_POLY);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 16; k++) pw[k] = 0;
+                        }
+                        tmem_st16_issue(t_s + c / 2, pw);
+                        if (c == 64) {
+                            tmem_st_wait();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&p_lo[w]);
+                        }
+                    }
+                }
                 float s0, s1, s2, s3;
                 pgt_unpack(sums[0], &s0, &s1);
                 pgt_unpack(sums[1], &s2, &s3);
@@ -447,15 +517,6 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                 uint32_t orow[32];
                 __syncwarp();                              // the load is the whole warp's
                 tmem_ld32(t_o + c, orow);
-                if (fix && real) {
-#pragma unroll 1
-                    for (int k = 0; k < 32; k++) {
-                        const float add = pg_nonfinite<KT>(p, pc, pos, c + k);
-#pragma unroll
-                        for (int k2 = 0; k2 < 32; k2++)
-                            if (k2 == k) orow[k2] = __float_as_uint(__uint_as_float(orow[k2]) + add);
-                    }
-                }
                 if (whole) {
                     // the block's queries are no longer needed (every S has been computed): their place takes the outputs
 #pragma unroll
@@ -473,6 +534,23 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
 #pragma unroll
                     for (int k = 0; k < 32; k += 4)
                         *reinterpret_cast<uint4*>(slot + ((size_t)((c + k) / 4) * M + rm) * 4) = make_uint4(orow[k], orow[k + 1], orow[k + 2], orow[k + 3]);
+                }
+            }
+            if (fix && real) {
+                // rare: what non-finite elements of V do to this row
+#pragma unroll 1
+                for (int e = 0; e < D; e++) {
+                    const float add = pg_nonfinite<KT>(p, pc, pos, e);
+                    if (add == 0.f) continue;
+                    if (whole) {
+                        const int oc = e / 8;
+                        uint8_t* d = oc < 8 * C::NA ? qd + (oc >> 3) * C::A_BYTES + lane * 128 + (((oc & 7) ^ (lane & 7)) << 4)
+                                                    : qd + C::NA * C::A_BYTES - quad * 32 * 64 + lane * 64 + (((oc & 3) ^ ((lane >> 1) & 3)) << 4);
+                        __nv_bfloat16* x = reinterpret_cast<__nv_bfloat16*>(d) + e % 8;
+                        *x = __float2bfloat16_rn(__bfloat162float(*x) + add);
+                    } else {
+                        slot[((size_t)(e / 4) * M + rm) * 4 + e % 4] += add;
+                    }
                 }
             }
             if (whole) {
