@@ -87,6 +87,15 @@ __device__ __noinline__ float pg_nonfinite(const PgAttend& p, const PgPiece& pc,
     return add;
 }
 
+// mbar_wait in few instructions: these kernels wait in many places, and their code competes for the instruction caches.
+__device__ __forceinline__ bool pg_wait(uint64_t* bar, uint32_t parity) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < TC_SPIN_LIMIT; i++) {
+        if (mbar_test(bar, parity)) return true;
+        if (i > 64) __nanosleep(64);
+    }
+    return false;
+}
 // One lane of a converged warp, the same every time.
 __device__ __forceinline__ bool elect_one() {
     uint32_t yes;
@@ -134,7 +143,7 @@ template <int KT, int DEPTH> struct PgProducer {
         PgPiece pc;
         const bool more = walk.next(p.ge.n_kv, &pc);
         const int s = qn % DEPTH;
-        if (empty && qn >= DEPTH && !mbar_wait(&empty[s], ((qn / DEPTH) - 1) & 1)) return false;
+        if (empty && qn >= DEPTH && !pg_wait(&empty[s], ((qn / DEPTH) - 1) & 1)) return false;
         if ((threadIdx.x & 31) == 0) {
             if (!more) pc.i1 = -1;
             queue[s] = pc;
@@ -222,7 +231,7 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
             const int i0 = q->i0, i1 = q->i1;
             for (int i = i0; i < i1; i++, cnt++) {
                 const int s = cnt % S, l0 = bx.tile_lane(p, q, i);
-                if (cnt >= S && !mbar_wait(&empty[s], ((cnt / S) - 1) & 1)) { ok = false; break; }
+                if (cnt >= S && !pg_wait(&empty[s], ((cnt / S) - 1) & 1)) { ok = false; break; }
                 uint8_t* dst = base + s * C::STAGE_BYTES;
                 if (issuer) mbar_expect_tx(&full[s], T::BYTES);
 #pragma unroll 1
@@ -240,7 +249,7 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
         if (!ok) *abort_flag = 1;
         if (__any_sync(0xffffffffu, bx.bad) && lane == 0) atomicOr(p.w.status, PG_ST_BAD_PAGE);
         if (*abort_flag)                                   // every copy lands before the block's memory is released
-            for (int c = max(0, cnt - S); c < cnt; c++) mbar_wait(&full[c % S], (c / S) & 1);
+            for (int c = max(0, cnt - S); c < cnt; c++) pg_wait(&full[c % S], (c / S) & 1);
         }
     } else {
         // ---- consumers ----
@@ -253,7 +262,7 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
         for (int qn = 0; ; qn++) {
             const int qs = qn % PGM_QUEUE;
             if (tid == 0) {
-                const bool got = !*abort_flag && mbar_wait(&q_full[qs], (qn / PGM_QUEUE) & 1);
+                const bool got = !*abort_flag && pg_wait(&q_full[qs], (qn / PGM_QUEUE) & 1);
                 if (!got) *abort_flag = 1;
                 stop_s = !got;
             }
@@ -288,7 +297,7 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
             const int len = pc.i1 - pc.i0;
             for (int t = (kg - cnt % WK + WK) % WK; t < len && ok; t += WK) {
                 const int c = cnt + t, s = c % S;
-                ok = mbar_wait(&full[s], (c / S) & 1) && !*abort_flag;
+                ok = pg_wait(&full[s], (c / S) & 1) && !*abort_flag;
                 if (!ok) break;
                 const uint8_t* Kt = ring + s * C::STAGE_BYTES;
                 const uint8_t* Vt = Kt + T::BYTES;

@@ -35,8 +35,9 @@ template <int D> struct PgtCfg {
     static constexpr int NA = D / 64, NB = (D % 64) / 32;
     static constexpr int A_BYTES = 128 * 128, B_BYTES = 128 * 64;        // 128 rows of 64 / 32 columns
     static constexpr int TILE = NA * A_BYTES + NB * B_BYTES;
-    static constexpr int STAGES = D == 128 ? 5 : D == 96 ? 7 : 10;
-    static constexpr int SMEM = 1024 + 2 * TILE + STAGES * TILE;
+    // K and V have stages of their own: whoever waits for one kind only then never waits two phases ahead
+    static constexpr int SK = D == 128 ? 2 : D == 96 ? 3 : 5, SV = D == 128 ? 3 : D == 96 ? 4 : 5;
+    static constexpr int SMEM = 1024 + (2 + SK + SV) * TILE;
     static constexpr int S_COL = 0, O_COL = 256;                         // + 128 for block B
 };
 
@@ -127,12 +128,13 @@ template <int D>
 __global__ void __launch_bounds__(PGT_THREADS, 1)
 pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ PgMaps maps) {
     using C = PgtCfg<D>;
-    constexpr int S = C::STAGES, M = PGT_M, KT = PGT_KT;
+    constexpr int SK = C::SK, SV = C::SV, M = PGT_M, KT = PGT_KT;
     extern __shared__ uint8_t pgt_raw[];
     uint8_t* Qs = (uint8_t*)(((uintptr_t)pgt_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t* ring = Qs + 2 * C::TILE;
+    uint8_t* ring_k = Qs + 2 * C::TILE;
+    uint8_t* ring_v = ring_k + SK * C::TILE;
     __shared__ PgPlanSmem<1> plan;
-    __shared__ uint64_t full[S], empty[S], clean[S], qu_full[PGT_QUEUE], qu_empty[PGT_QUEUE];
+    __shared__ uint64_t k_full[SK], k_empty[SK], v_full[SV], v_empty[SV], v_clean[SV], qu_full[PGT_QUEUE], qu_empty[PGT_QUEUE];
     __shared__ uint64_t q_full[2], s_full[2], p_lo[2], p_hi[2], o_full[2];     // P in two parts: 96 keys, 32 keys
     __shared__ PgPiece queue[PGT_QUEUE], queue_v[PGT_QUEUE];
     __shared__ int found[PGT_QUEUE];
@@ -142,7 +144,8 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int s = 0; s < S; s++) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); mbar_init(&clean[s], 1); }
+        for (int s = 0; s < SK; s++) { mbar_init(&k_full[s], 1); mbar_init(&k_empty[s], 1); }
+        for (int s = 0; s < SV; s++) { mbar_init(&v_full[s], 1); mbar_init(&v_empty[s], 1); mbar_init(&v_clean[s], 1); }
         for (int s = 0; s < PGT_QUEUE; s++) { mbar_init(&qu_full[s], 1); mbar_init(&qu_empty[s], 10); }
         for (int w = 0; w < 2; w++) { mbar_init(&q_full[w], 4); mbar_init(&s_full[w], 1); mbar_init(&p_lo[w], 4); mbar_init(&p_hi[w], 4); mbar_init(&o_full[w], 1); }
         abort_s = 0;
@@ -159,22 +162,25 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
     if (warp >= 8) {
         pg_regs_less<PG_REGS_LESS>();
         if (warp == 8 || warp == 10) {
-        // ---- producers: K(0) V(0) K(1) V(1) ... of every piece, warp 8 the K tiles (and the queue), warp 10 the V tiles ----
+        // ---- producers: warp 8 the K tiles (and the queue), warp 10 the V tiles ----
         const int kv = warp == 10;
         PgProducer<KT, PGT_QUEUE> bx;
         bx.queue = kv ? queue_v : queue; bx.full = kv ? nullptr : qu_full; bx.empty = kv ? nullptr : qu_empty; bx.found = kv ? nullptr : found;
         bool ok = bx.start(p, plan);
         const bool issuer = elect_one();
         const CUtensorMap *m64 = kv ? &maps.v64 : &maps.k64, *m32 = kv ? &maps.v32 : &maps.k32;
+        uint8_t* const ring = kv ? ring_v : ring_k;
+        uint64_t *const full = kv ? v_full : k_full, *const empty = kv ? v_empty : k_empty;
         const int nbox = 1 << bx.lg_box;
-        int cnt = kv;
+        int cnt = 0, s = 0;                                // tiles asked for, stage of the next one
+        uint32_t ph = 1;                                   // parity of the phase that frees it (the first round is free)
         while (ok) {
             const PgPiece* q = bx.begin(p);
             if (!q) break;
             const int i0 = q->i0, i1 = q->i1;
-            for (int i = i0; i < i1; i++, cnt += 2) {
-                const int s = cnt % S, l0 = bx.tile_lane(p, q, i);
-                if (cnt >= S && !mbar_wait(&empty[s], ((cnt / S) - 1) & 1)) { ok = false; break; }
+            for (int i = i0; i < i1; i++) {
+                const int l0 = bx.tile_lane(p, q, i);
+                if (!pg_wait(&empty[s], ph)) { ok = false; break; }
                 uint8_t* d = ring + s * C::TILE;
                 if (issuer) mbar_expect_tx(&full[s], C::TILE);
 #pragma unroll 1
@@ -186,29 +192,31 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                         if (C::NB) tma_load_2d(d + C::NA * C::A_BYTES + at * 64, m32, C::NA * 64, y, &full[s]);
                     }
                 }
-                if (i == i0 && !bx.push(p)) { cnt += 2; ok = false; break; }
+                cnt++;
+                if (++s == (kv ? SV : SK)) { s = 0; ph ^= 1; }
+                if (i == i0 && !bx.push(p)) { ok = false; break; }
             }
         }
         if (!ok) *abort_flag = 1;
         if (__any_sync(0xffffffffu, bx.bad) && lane == 0) atomicOr(p.w.status, PG_ST_BAD_PAGE);
         if (*abort_flag)
-            for (int c = cnt - 2; c >= max(0, cnt - S); c -= 2) mbar_wait(&full[c % S], (c / S) & 1);
+            for (int c = max(0, cnt - (kv ? SV : SK)); c < cnt; c++) pg_wait(&full[c % (kv ? SV : SK)], (c / (kv ? SV : SK)) & 1);
         } else if (warp == 11) {
         // ---- V tiles that some row does not see all of: non-finite elements out, before anyone multiplies by them ----
-        int cnt = 1;
+        int cnt = 0;
         bool ok = true;
         for (int qn = 0; ok; qn++) {
             const int qs = qn % PGT_QUEUE;
-            ok = !*abort_flag && mbar_wait(&qu_full[qs], (qn / PGT_QUEUE) & 1);
+            ok = !*abort_flag && pg_wait(&qu_full[qs], (qn / PGT_QUEUE) & 1);
             if (!ok) break;
             const PgPiece pc = queue[qs];
             if (pc.i1 < 0) break;
             const PgSpan span = pg_span<KT>(pc.pmin, pc.pmax, p.window, p.sinks);
-            for (int i = pc.i0; i < pc.i1 && ok; i++, cnt += 2) {
-                const int s = cnt % S;
-                ok = mbar_wait(&full[s], (cnt / S) & 1);
+            for (int i = pc.i0; i < pc.i1 && ok; i++, cnt++) {
+                const int s = cnt % SV;
+                ok = pg_wait(&v_full[s], (cnt / SV) & 1);
                 if (ok && pg_partial<KT>(pg_tile_key(span, i, KT), pc.pmin, pc.pmax, p.window, p.sinks)) {
-                    uint8_t* vt = ring + s * C::TILE;
+                    uint8_t* vt = ring_v + s * C::TILE;
                     // 16-byte chunks in the order they lie in: D * 128 / 8 of them, the same for every swizzle
                     uint32_t seen = 0;
 #pragma unroll 8
@@ -218,7 +226,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                                 ((v.z & 0x7f807f80u) + 0x00800080u) | ((v.w & 0x7f807f80u) + 0x00800080u);
                     }
                     if (seen & 0x80008000u) {
-                        bool hit;
+                        bool hit = false;
                         for (int c = lane; c < C::TILE / 16; c += 32) {
                             uint4 v = *reinterpret_cast<const uint4*>(vt + c * 16);
                             v.x = pgm_finite(v.x, &hit); v.y = pgm_finite(v.y, &hit); v.z = pgm_finite(v.z, &hit); v.w = pgm_finite(v.w, &hit);
@@ -230,7 +238,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 __syncwarp();
-                if (ok && lane == 0) mbar_arrive(&clean[s]);
+                if (ok && lane == 0) mbar_arrive(&v_clean[s]);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&qu_empty[qs]);
@@ -241,20 +249,20 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
         constexpr uint32_t idesc_s = umma_idesc(KT);
         constexpr uint32_t idesc_o = umma_idesc_bmn(C::NB ? 64 * C::NA : D);
         constexpr uint32_t idesc_o32 = umma_idesc_bmn(32);
-        const uint32_t q0 = smem_u32(Qs), r0 = smem_u32(ring);
+        const uint32_t q0 = smem_u32(Qs), rk = smem_u32(ring_k), rv = smem_u32(ring_v);
         int cnt = 0;
         uint32_t np[2] = {0, 0}, ns = 0;                   // P tiles consumed per block, pieces seen
         bool ok = true;
         for (int qn = 0; ok; qn++) {
             const int qs = qn % PGT_QUEUE;
-            ok = !*abort_flag && mbar_wait(&qu_full[qs], (qn / PGT_QUEUE) & 1);
+            ok = !*abort_flag && pg_wait(&qu_full[qs], (qn / PGT_QUEUE) & 1);
             if (!ok) break;
             const PgPiece pc = queue[qs];
             if (pc.i1 < 0) break;
             const int len = pc.i1 - pc.i0;
             const int nb = (unsigned)pc.n * p.ge.g - (unsigned)pc.rt * M > 128u ? 2 : 1;
-            auto qk = [&](int w, int c) {                  // S_w = Q_w K^T, K in load number c
-                const uint32_t k0 = r0 + (c % S) * C::TILE, qw = q0 + w * C::TILE, d = tmem + C::S_COL + w * 128;
+            auto qk = [&](int w, int c) {                  // S_w = Q_w K^T, K tile number c of the block
+                const uint32_t k0 = rk + (c % SK) * C::TILE, qw = q0 + w * C::TILE, d = tmem + C::S_COL + w * 128;
                 tc_fence_after();
 #pragma unroll
                 for (int a = 0; a < C::NA; a++)
@@ -269,8 +277,8 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                                   umma_desc_k64(k0 + C::NA * C::A_BYTES) + (uint64_t)(k * 2), idesc_s, 1u);
                 }
             };
-            auto pv = [&](int w, int c, bool first, int k0, int k1) {      // O_w += P_w V over keys 16 k0 .. 16 k1, V in load number c
-                const uint32_t v0 = r0 + (c % S) * C::TILE, a0 = tmem + C::S_COL + w * 128, d = tmem + C::O_COL + w * 128;
+            auto pv = [&](int w, int c, bool first, int k0, int k1) {      // O_w += P_w V over keys 16 k0 .. 16 k1, V tile number c
+                const uint32_t v0 = rv + (c % SV) * C::TILE, a0 = tmem + C::S_COL + w * 128, d = tmem + C::O_COL + w * 128;
                 tc_fence_after();
 #pragma unroll
                 for (int k = k0; k < k1; k++)
@@ -281,45 +289,45 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                         umma_bf16_ts(d + C::NA * 64, a0 + k * 8, umma_desc_mn64(v0 + C::NA * C::A_BYTES + k * 1024), idesc_o32, (!first || k) ? 1u : 0u);
                 }
             };
-            // uses of a stage by V tiles before load c: every use where K and V keep to their stages (S even), every other one else
-            auto v_phase = [](int c) { return (uint32_t)(S % 2 ? (c / S) >> 1 : c / S) & 1u; };
             const bool issuer = elect_one();
-            ok = mbar_wait(&full[cnt % S], (cnt / S) & 1);
+            ok = pg_wait(&k_full[cnt % SK], (cnt / SK) & 1);
             for (int w = 0; w < nb && ok; w++) {
-                ok = !*abort_flag && mbar_wait(&q_full[w], ns & 1);
+                ok = !*abort_flag && pg_wait(&q_full[w], ns & 1);
                 if (ok && issuer) {
                     qk(w, cnt);
                     umma_commit(&s_full[w]);
-                    if (w == nb - 1) umma_commit(&empty[cnt % S]);      // K(0)
+                    if (w == nb - 1) umma_commit(&k_empty[cnt % SK]);      // K(0)
                 }
             }
             for (int j = 0; j < len && ok; j++) {
-                const int cv = cnt + 2 * j + 1, ck = cv + 1;
+                const int cv = cnt + j, ck = cv + 1;
                 const bool more = j + 1 < len;
-                ok = mbar_wait(&clean[cv % S], v_phase(cv)) && (!more || mbar_wait(&full[ck % S], (ck / S) & 1));
+                ok = pg_wait(&v_clean[cv % SV], (cv / SV) & 1) && (!more || pg_wait(&k_full[ck % SK], (ck / SK) & 1));
                 for (int w = 0; w < nb && ok; w++) {
-                    ok = !*abort_flag && mbar_wait(&p_lo[w], np[w] & 1);
+                    ok = !*abort_flag && pg_wait(&p_lo[w], np[w] & 1);
                     if (ok && issuer) pv(w, cv, j == 0, 0, 6);
                     __syncwarp();
-                    ok = ok && mbar_wait(&p_hi[w], np[w] & 1);
+                    ok = ok && pg_wait(&p_hi[w], np[w] & 1);
                     np[w]++;
                     if (ok && issuer) {
                         pv(w, cv, false, 6, 8);
-                        if (w == nb - 1) umma_commit(&empty[cv % S]);
+                        if (w == nb - 1) umma_commit(&v_empty[cv % SV]);
                         if (more) {
                             qk(w, ck);
                             umma_commit(&s_full[w]);
-                            if (w == nb - 1) umma_commit(&empty[ck % S]);
+                            if (w == nb - 1) umma_commit(&k_empty[ck % SK]);
                         } else {
                             umma_commit(&o_full[w]);
                         }
                     }
+                    __syncwarp();
                 }
             }
+            if (ok && nb == 1) ok = pg_wait(&q_full[1], ns & 1);     // no phase of a barrier is left out (block B arrives, too)
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) *abort_flag = 1;
             __syncwarp();
-            cnt += 2 * len;
+            cnt += len;
             ns++;
             if (lane == 0) mbar_arrive(&qu_empty[qs]);
         }
@@ -337,7 +345,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
         bool ok = true;
         for (int qn = 0; ok; qn++) {
             const int qs = qn % PGT_QUEUE;
-            ok = !*abort_flag && mbar_wait(&qu_full[qs], (qn / PGT_QUEUE) & 1);
+            ok = !*abort_flag && pg_wait(&qu_full[qs], (qn / PGT_QUEUE) & 1);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             const PgPiece pc = queue[qs];
@@ -383,7 +391,7 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
             const int lo = pg_window_lo(pos, p.window);
             float m = -INFINITY, l = 0.f;                  // m: the maximum (log2 domain) the row's P and O are scaled by
             for (int j = 0; j < len; j++) {
-                ok = !*abort_flag && mbar_wait(&s_full[w], n_s & 1);
+                ok = !*abort_flag && pg_wait(&s_full[w], n_s & 1);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 n_s++;
@@ -502,7 +510,7 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_hi[w]);
             }
-            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&o_full[w], n_o & 1));
+            if (ok) ok = __all_sync(0xffffffffu, pg_wait(&o_full[w], n_o & 1));
             n_o++;
             if (!ok) { *abort_flag = 1; break; }
             tc_fence_after();
