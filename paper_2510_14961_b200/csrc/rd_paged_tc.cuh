@@ -251,7 +251,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
         constexpr uint32_t idesc_o32 = umma_idesc_bmn(32);
         const uint32_t q0 = smem_u32(Qs), rk = smem_u32(ring_k), rv = smem_u32(ring_v);
         int cnt = 0;
-        uint32_t np[2] = {0, 0}, ns = 0;                   // P tiles consumed per block, pieces seen
+        uint32_t np[2] = {0, 0}, nq[2] = {0, 0};           // per block: P tiles consumed, queries multiplied
         bool ok = true;
         for (int qn = 0; ok; qn++) {
             const int qs = qn % PGT_QUEUE;
@@ -292,7 +292,8 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
             const bool issuer = elect_one();
             ok = pg_wait(&k_full[cnt % SK], (cnt / SK) & 1);
             for (int w = 0; w < nb && ok; w++) {
-                ok = !*abort_flag && pg_wait(&q_full[w], ns & 1);
+                ok = !*abort_flag && pg_wait(&q_full[w], nq[w] & 1);
+                nq[w]++;
                 if (ok && issuer) {
                     qk(w, cnt);
                     umma_commit(&s_full[w]);
@@ -323,12 +324,10 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
                     __syncwarp();
                 }
             }
-            if (ok && nb == 1) ok = pg_wait(&q_full[1], ns & 1);     // no phase of a barrier is left out (block B arrives, too)
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) *abort_flag = 1;
             __syncwarp();
             cnt += len;
-            ns++;
             if (lane == 0) mbar_arrive(&qu_empty[qs]);
         }
         if (!ok) *abort_flag = 1;
@@ -360,7 +359,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
             if (pos >= limit) pos = -1;
             if (w == 1 && packed - (unsigned)pc.rt * M <= 128u) {             // block B is empty
                 __syncwarp();
-                if (lane == 0) { mbar_arrive(&q_full[1]); mbar_arrive(&qu_empty[qs]); }
+                if (lane == 0) mbar_arrive(&qu_empty[qs]);
                 continue;
             }
             // the warp's 32 queries into the block's operand tile: D / 8 lanes share a row (whole lines from memory)
