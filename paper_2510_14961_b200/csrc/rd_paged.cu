@@ -125,15 +125,17 @@ static int create_impl(rd_paged* c, void* k, void* v) {
         PTRY(encode_set(&c->maps_many, c->k, c->v, pool_rows, g.head_dim, std::min(g.page_size, PGT_KT)));
     }
     // workspace: status | counters a | counters b | n_rec a, b | records a | records b | partial results a | b
-    const int nb = c->n_sms, grp = g.n_heads / g.n_kv_heads, mb = c->tensor ? PGT_M : PGS_MANY;
+    const int nb = 2 * c->n_sms, grp = g.n_heads / g.n_kv_heads, mb = c->tensor ? PGT_M : PGS_MANY;
     const long long packed = (long long)g.max_rows * grp;
     c->cap_a = (int)std::min<long long>(PG_MAX_GROUPS + packed / 16 + 1, 1 << 28);
     c->cap_b = (int)std::min<long long>(PG_MAX_GROUPS + packed / 64 + 1, 1 << 28);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-    const size_t o_st = take(256), o_ca = take((size_t)nb * 4), o_cb = take((size_t)nb * 8 * 4);
+    const size_t o_st = take(256), o_ca = take((size_t)nb * 4), o_cb = take((size_t)nb * 8 * 4);     // (at most two blocks per SM)
     const size_t o_ra = take((size_t)c->cap_a * sizeof(PgRecord)), o_rb = take((size_t)c->cap_b * sizeof(PgRecord));
-    const size_t o_pa = take((size_t)2 * nb * 64 * (g.head_dim + 2) * 4), o_pb = take((size_t)2 * nb * mb * (g.head_dim + 2) * 4);
+    // the kernels on tensor cores run one block per SM, the others up to two
+    const size_t slots = 2 * (size_t)(c->tensor ? c->n_sms : nb);
+    const size_t o_pa = take(slots * 64 * (g.head_dim + 2) * 4), o_pb = take(slots * mb * (g.head_dim + 2) * 4);
     PCU(cudaMalloc((void**)&c->work, at));
     PCU(cudaMemset(c->work, 0, o_ra));
     c->status = (int*)(c->work + o_st);
@@ -216,7 +218,7 @@ int rd::paged_append_sums(rd_paged* c, const PgBatch& b, int layer, const RowSou
 }
 
 // One attention launch: the plan (inside the kernel while it is small, else a kernel in front), then the kernel.
-struct AttendShape { int M, threads, kt; };
+struct AttendShape { int M, threads, per_sm; };
 template <int KT, typename Kern, typename... Extra>
 static int attend_launch(rd_paged* c, PgAttend a, bool part_b, const AttendShape& s, bool can_inline, Kern kern, int smem, cudaStream_t st,
                          bool chained, int* launches, const Extra&... extra) {
@@ -233,21 +235,21 @@ static int attend_launch(rd_paged* c, PgAttend a, bool part_b, const AttendShape
         PCU(launch_chained(pg_plan_kernel<KT>, dim3(blocks), dim3(PG_PLAN_THREADS), (size_t)a.b.n_groups * sizeof(int), st, chained, a, s.M));
         if (launches) ++*launches;
     }
-    PCU(launch_chained(kern, dim3(c->n_sms), dim3(s.threads), (size_t)smem, st, chained, a, extra...));
+    PCU(launch_chained(kern, dim3(c->n_sms * s.per_sm), dim3(s.threads), (size_t)smem, st, chained, a, extra...));
     if (launches) ++*launches;
     return RD_OK;
 }
 template <int D> static int attend_few_tensor(rd_paged* c, const PgAttend& a, int m, cudaStream_t st, bool chained, int* launches) {
-    if (m <= 16) return attend_launch<PGM_KT>(c, a, false, {16, PGM_THREADS, PGM_KT}, true, pg_attend_mma_kernel<D, 1>, PgmCfg<D, 1>::SMEM, st, chained, launches, c->maps_few);
-    if (m <= 32) return attend_launch<PGM_KT>(c, a, false, {32, PGM_THREADS, PGM_KT}, true, pg_attend_mma_kernel<D, 2>, PgmCfg<D, 2>::SMEM, st, chained, launches, c->maps_few);
-    return attend_launch<PGM_KT>(c, a, false, {64, PGM_THREADS, PGM_KT}, true, pg_attend_mma_kernel<D, 4>, PgmCfg<D, 4>::SMEM, st, chained, launches, c->maps_few);
+    if (m <= 16) return attend_launch<PGM_KT>(c, a, false, {16, PGM_THREADS, 1}, true, pg_attend_mma_kernel<D, 1>, PgmCfg<D, 1>::SMEM, st, chained, launches, c->maps_few);
+    if (m <= 32) return attend_launch<PGM_KT>(c, a, false, {32, PGM_THREADS, 1}, true, pg_attend_mma_kernel<D, 2>, PgmCfg<D, 2>::SMEM, st, chained, launches, c->maps_few);
+    return attend_launch<PGM_KT>(c, a, false, {64, PGM_THREADS, 1}, true, pg_attend_mma_kernel<D, 4>, PgmCfg<D, 4>::SMEM, st, chained, launches, c->maps_few);
 }
 template <int D> static int attend_many_tensor(rd_paged* c, const PgAttend& a, cudaStream_t st, bool chained, int* launches) {
-    return attend_launch<PGT_KT>(c, a, true, {PGT_M, PGT_THREADS, PGT_KT}, false, pg_attend_tc_kernel<D>, PgtCfg<D>::SMEM, st, chained, launches, c->maps_many);
+    return attend_launch<PGT_KT>(c, a, true, {PGT_M, PGT_THREADS, 1}, false, pg_attend_tc_kernel<D>, PgtCfg<D>::SMEM, st, chained, launches, c->maps_many);
 }
 template <typename T, int DP> static int attend_simt(rd_paged* c, const PgAttend& a, bool many, cudaStream_t st, bool chained, int* launches) {
-    if (!many) return attend_launch<PGS_KT>(c, a, false, {PGS_FEW, PGS_THREADS, PGS_KT}, true, pg_attend_few_kernel<T, DP>, PgsFew<T, DP>::SMEM, st, chained, launches);
-    return attend_launch<PGS_KT>(c, a, true, {PGS_MANY, PGS_THREADS, PGS_KT}, true, pg_attend_many_kernel<T, DP>, PgsMany<T, DP>::SMEM, st, chained, launches);
+    if (!many) return attend_launch<PGS_KT>(c, a, false, {PGS_FEW, PGS_THREADS, 1}, true, pg_attend_few_kernel<T, DP>, PgsFew<T, DP>::SMEM, st, chained, launches);
+    return attend_launch<PGS_KT>(c, a, true, {PGS_MANY, PGS_THREADS, PgsMany<T, DP>::PER_SM}, true, pg_attend_many_kernel<T, DP>, PgsMany<T, DP>::SMEM, st, chained, launches);
 }
 template <typename T> static int attend_simt_d(rd_paged* c, const PgAttend& a, bool many, cudaStream_t st, bool chained, int* launches) {
     if (a.ge.D <= 32) return attend_simt<T, 32>(c, a, many, st, chained, launches);

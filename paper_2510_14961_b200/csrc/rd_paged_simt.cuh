@@ -44,13 +44,26 @@ __device__ __forceinline__ void pgs_row_in(T* dst, const T* src, int D, int c0, 
         for (int c = c0; c < D; c += step) dst[c] = src[c];
     }
 }
-// Row of the pages that holds `key`, clamped to a page that exists (status raised: results are then meaningless).
-__device__ __forceinline__ long long pgs_row(const PgAttend& p, int grp, int head, int key, bool* bad) {
-    const long long r = pg_row_of(p.b, p.ge, grp, head, key);
-    if (r >= 0) return r;
-    *bad = true;
-    return 0;
-}
+// Where a thread's key of successive tiles lies: the table entry is asked for a tile ahead of its use, so that no
+// copy waits for one.  row < 0: a key no row sees (it is not read: it may lie beyond the sequence's pages).
+struct PgsKey {
+    int next_key, entry;                                   // key of the next tile (-1: none), its table entry
+    bool bad;
+    __device__ __forceinline__ void ask(const PgAttend& p, const PgPiece& pc, const PgSpan& span, int lo_key, int i, int offset) {
+        next_key = -1;
+        if (i < pc.i1) {
+            const int key = pg_tile_key(span, i, 64) + offset;
+            if (key <= pc.pmax && (key >= lo_key || key < p.sinks)) next_key = key;
+        }
+        const int pi = next_key >> p.ge.page_shift;
+        entry = next_key >= 0 && pi < p.b.table_stride ? p.b.table[(size_t)pc.grp * p.b.table_stride + pi] : -1;
+    }
+    __device__ __forceinline__ long long row(const PgAttend& p, const PgPiece& pc) {
+        if (next_key < 0) return -1;
+        if (entry < 0 || entry >= p.ge.n_pages) { bad = true; return -1; }      // (results of such rows are undefined)
+        return ((((long long)p.ge.layer * p.ge.n_pages + entry) * p.ge.n_kv + pc.head) << p.ge.page_shift) + (next_key & ((1 << p.ge.page_shift) - 1));
+    }
+};
 __device__ __forceinline__ int pgs_row_position(const PgAttend& p, const PgPiece& pc, int M, int r, int limit) {
     const long long pk = (long long)pc.rt * M + r;
     if (r >= M || pk >= (long long)pc.n * p.ge.g) return -1;
@@ -84,7 +97,8 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_few_kernel(const __g
     const int limit = pg_pos_limit(p.b, p.ge);
     T* mine = reinterpret_cast<T*>(ring + warp * S * 2 * C::RUN);
     const int key_l = lane >> 2, quarter = lane & 3;
-    bool bad = false;
+    PgsKey key;
+    key.bad = false;
     auto sync = [] { __syncthreads(); };
     PgWalk walk;
     walk.start(p, plan);
@@ -105,19 +119,16 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_few_kernel(const __g
             Qs[r * QLD + e] = x;
         }
         __syncthreads();
+        key.ask(p, pc, span, lo_key, pc.i0, warp * C::KEYS + key_l);
         auto issue = [&](int i) {                                  // tile i's run of this warp into stage (i - i0) % S
-            if (i < pc.i1) {
-                const int key0 = pg_tile_key(span, i, PGS_KT) + warp * C::KEYS;
-                T* kd = mine + (size_t)((i - pc.i0) % S) * 2 * C::KEYS * LD;
-                const int key = key0 + key_l;
-                // keys no row sees are not read: they may lie beyond the sequence's pages
-                if (key <= pc.pmax && (key >= lo_key || key < p.sinks)) {
-                    const size_t row = (size_t)pgs_row(p, pc.grp, pc.head, key, &bad) * D;
-                    pgs_row_in(kd + key_l * LD, (const T*)p.k + row, D, quarter, 4);
-                    pgs_row_in(kd + (C::KEYS + key_l) * LD, (const T*)p.v + row, D, quarter, 4);
-                }
+            T* kd = mine + (size_t)((i - pc.i0) % S) * 2 * C::KEYS * LD;
+            const long long row = key.row(p, pc);
+            if (row >= 0) {
+                pgs_row_in(kd + key_l * LD, (const T*)p.k + (size_t)row * D, D, quarter, 4);
+                pgs_row_in(kd + (C::KEYS + key_l) * LD, (const T*)p.v + (size_t)row * D, D, quarter, 4);
             }
             pgs_commit();
+            key.ask(p, pc, span, lo_key, i + 1, warp * C::KEYS + key_l);
         };
         int pos[M];
 #pragma unroll
@@ -217,7 +228,7 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_few_kernel(const __g
         if (!whole && pg_arrive_last(p.w, pc, tid == 0, &flag, sync)) pg_join_any<T>(p, pc, M, D, tid, PGS_THREADS);
         __syncthreads();
     }
-    if (bad) atomicOr(p.w.status, PG_ST_BAD_PAGE);
+    if (key.bad) atomicOr(p.w.status, PG_ST_BAD_PAGE);
 }
 
 template <typename T, int DP> struct PgsMany {
@@ -225,10 +236,12 @@ template <typename T, int DP> struct PgsMany {
     static constexpr int TILE = PGS_KT * LD * (int)sizeof(T);
     static constexpr int QLD = DP + 4, PLD = PGS_KT + 4;
     static constexpr int SMEM = 2 * TILE + PGS_MANY * QLD * 4 + PGS_MANY * PLD * 4;
+    static constexpr int PER_SM = DP <= 64 ? 2 : 1;
 };
 
+// Two blocks share an SM where their tiles fit (head_dim up to 64): one block's barriers hide behind the other's work.
 template <typename T, int DP>
-__global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_many_kernel(const __grid_constant__ PgAttend p) {
+__global__ void __launch_bounds__(PGS_THREADS, PgsMany<T, DP>::PER_SM) pg_attend_many_kernel(const __grid_constant__ PgAttend p) {
     using C = PgsMany<T, DP>;
     constexpr int M = PGS_MANY, LD = C::LD, QLD = C::QLD, PLD = C::PLD, E = DP / 32, RW = 8;
     extern __shared__ __align__(16) uint8_t pgs_raw[];
@@ -241,8 +254,9 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_many_kernel(const __
     pdl_enter();
     pg_plan_share<PGS_THREADS, PGS_KT>(p, M, plan);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, D = p.ge.D;
-    const int limit = pg_pos_limit(p.b, p.ge), r_w = warp * RW;
-    bool bad = false;
+    const int limit = pg_pos_limit(p.b, p.ge), r_w = warp * RW, kl = tid >> 2;
+    PgsKey key;
+    key.bad = false;
     auto sync = [] { __syncthreads(); };
     for (int i = tid; i < 2 * C::TILE / 16; i += PGS_THREADS) reinterpret_cast<uint4*>(pgs_raw)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
@@ -253,17 +267,21 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_many_kernel(const __
         const PgSpan span = pg_span<PGS_KT>(pc.pmin, pc.pmax, p.window, p.sinks);
         const int rows = (int)min((long long)M, (long long)pc.n * p.ge.g - (long long)pc.rt * M);
         const int lo_key = p.window > 0 ? max(0, pc.pmin - p.window + 1) : 0;
-        // four threads bring one key's row in
-        auto load = [&](T* dst, const void* pages, int i) {
-            if (i < pc.i1) {
-                const int kl = tid >> 2, key = pg_tile_key(span, i, PGS_KT) + kl;
-                if (key <= pc.pmax && (key >= lo_key || key < p.sinks))
-                    pgs_row_in(dst + kl * LD, (const T*)pages + (size_t)pgs_row(p, pc.grp, pc.head, key, &bad) * D, D, tid & 3, 4);
-            }
+        // four threads bring one key's row in; `row` is where the tile whose K was asked for last lies
+        key.ask(p, pc, span, lo_key, pc.i0, kl);
+        long long row_k = -1;
+        auto load_k = [&](int i) {
+            row_k = key.row(p, pc);
+            if (row_k >= 0) pgs_row_in(Ks + kl * LD, (const T*)p.k + (size_t)row_k * D, D, tid & 3, 4);
+            pgs_commit();
+            key.ask(p, pc, span, lo_key, i + 1, kl);
+        };
+        auto load_v = [&]() {
+            if (row_k >= 0) pgs_row_in(Vs + kl * LD, (const T*)p.v + (size_t)row_k * D, D, tid & 3, 4);
             pgs_commit();
         };
-        load(Ks, p.k, pc.i0);
-        load(Vs, p.v, pc.i0);
+        load_k(pc.i0);
+        load_v();
         for (int i = tid; i < M * DP; i += PGS_THREADS) {
             const int r = i / DP, e = i % DP;
             float x = 0.f;
@@ -307,7 +325,7 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_many_kernel(const __
                 }
             }
             __syncthreads();                                       // K(i) has been read
-            load(Ks, p.k, i + 1);
+            load_k(i + 1);
             if (work) {
 #pragma unroll
                 for (int r = 0; r < RW; r++) {
@@ -332,9 +350,18 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_many_kernel(const __
             pgs_wait<1>();
             __syncthreads();                                       // V(i) is there (and the warp's own P)
             if (work) {
-                // tiles with a key that some row does not see go key by key (0 times an infinity would be a NaN), the others
-                // four keys at a time
-                if (!pg_partial<PGS_KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks)) {
+                // four keys at a time; a tile with a key that some row does not see goes key by key when V is not finite all
+                // over it (0 times an infinity would be a NaN)
+                bool fast = true;
+                if (pg_partial<PGS_KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks)) {
+                    float probe = 0.f;
+#pragma unroll 4
+                    for (int j = 0; j < PGS_KT; j++)
+#pragma unroll
+                        for (int e = 0; e < E; e++) probe = fmaf(pg_to_f(Vs[j * LD + lane + 32 * e]), 0.f, probe);
+                    fast = __all_sync(0xffffffffu, probe == 0.f);
+                }
+                if (fast) {
 #pragma unroll 2
                     for (int j = 0; j < PGS_KT; j += 4) {
                         float v[4][E];
@@ -366,7 +393,7 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_many_kernel(const __
                 }
             }
             __syncthreads();                                       // V(i) has been read
-            load(Vs, p.v, i + 1);
+            load_v();
         }
         pgs_wait<0>();
         const bool whole = pc.c_first == pc.c_last;
@@ -396,7 +423,7 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_many_kernel(const __
         if (!whole && pg_arrive_last(p.w, pc, tid == 0, &flag, sync)) pg_join_any<T>(p, pc, M, D, tid, PGS_THREADS);
         __syncthreads();
     }
-    if (bad) atomicOr(p.w.status, PG_ST_BAD_PAGE);
+    if (key.bad) atomicOr(p.w.status, PG_ST_BAD_PAGE);
 }
 
 }  // namespace rd
