@@ -414,6 +414,26 @@ int rd_paged_attend(rd_paged* c, const rd_paged_rows* rows, int32_t layer, const
  * destroy the cache). */
 int rd_paged_sync(rd_paged* c, void* cuda_stream);
 
+/* rd_session_create_paged -- rd_session_create with the K/V caches in pages instead of max_context positions
+ * reserved for every sequence: pools of n_pages pages per layer of every block, one page table per
+ * sequence shared by all layers.  rd_prefill / rd_prefill_sliced reserve the pages of n_prompt + max_new_tokens
+ * positions for the sequence (returning those it held; CAPACITY, with nothing changed, when the pool has too few),
+ * so n_pages bounds the positions of all sequences together, and max_context those of one.
+ * rd_session_release stops a sequence and returns its pages; its tokens can no longer be read.
+ *   window, sinks  0, 0: every row attends all positions up to its own (the model of the paper).  window > 0: only
+ *                 the newest `window` positions and the first `sinks` (long generations at bounded cost; not in the paper).
+ * latent_slots below batch * max_window is refused (INVALID_ARG), rd_set_attention_path answers STATE; every
+ * other call works as for rd_session_create.  Errors of rd_session_release: INVALID_ARG, STATE (not a paged session, or
+ * a sliced prefill of the sequence is pending), CUDA. */
+typedef struct {
+    int32_t page_size;   /* as in rd_paged_config                                              */
+    int32_t n_pages;     /* pages of a layer's pool                                            */
+    int32_t window, sinks;
+} rd_paged_session_config;
+int rd_session_create_paged(const rd_model* m, const rd_session_config* sc, const rd_paged_session_config* pc, void* cuda_stream,
+                            rd_session** out);
+int rd_session_release(rd_session* s, int32_t seq);
+
 const char* rd_strerror(int code);
 /* Text of the last CUDA error this library saw on the calling thread's most recent failing call
  * (static storage, never NULL). */

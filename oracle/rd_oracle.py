@@ -187,6 +187,8 @@ class RDConfig:
     norm_eps: float = 1e-6
     init_sigma: float = 1.0
     tie_embeddings: bool = True
+    attn_window: int = 0      # > 0: a row attends its newest `attn_window` positions and the first `attn_sinks` only
+    attn_sinks: int = 0       # (not in the paper; 0: every position up to its own)
 
 
 def bf16_round(x):
@@ -272,11 +274,16 @@ class RDModel:
         scale = 1.0 / math.sqrt(d)
         for i in range(n):
             m = int(pos[i]) + 1
-            s = np.einsum("hd,mhd->hm", q[i], cache.K[l, :m]) * scale
+            K, V = cache.K[l, :m], cache.V[l, :m]
+            if c.attn_window > 0:
+                j = np.arange(m)
+                seen = (j > m - 1 - c.attn_window) | (j < c.attn_sinks)
+                K, V = K[seen], V[seen]
+            s = np.einsum("hd,mhd->hm", q[i], K) * scale
             s = s - s.max(axis=1, keepdims=True)
             pr = np.exp(s)
             pr = pr / pr.sum(axis=1, keepdims=True)
-            o[i] = np.einsum("hm,mhd->hd", pr, cache.V[l, :m])
+            o[i] = np.einsum("hm,mhd->hd", pr, V)
         x = x + self._q(o.reshape(n, H * d)) @ w[p + "wo"].T
         m2 = self._q(rmsnorm(x, w[p + "g2"], c.norm_eps))
         g = m2 @ w[p + "wg"].T

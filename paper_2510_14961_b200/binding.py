@@ -21,7 +21,7 @@ EXPORTS = ["rd_load", "rd_free", "rd_session_create", "rd_session_destroy", "rd_
            "rd_debug_expire_next_wait", "rd_set_fused_swiglu", "rd_set_attention_path", "rd_poll_begin", "rd_poll_end",
            "rd_debug_gemm_sequence", "rd_prefill_sliced", "rd_prefill_advance", "rd_prefill_pending",
            "rd_set_prefill_units", "rd_paged_create", "rd_paged_destroy", "rd_paged_pages", "rd_paged_append", "rd_paged_attend",
-           "rd_paged_sync"]
+           "rd_paged_sync", "rd_session_create_paged", "rd_session_release"]
 
 
 class RdConfig(C.Structure):
@@ -45,6 +45,10 @@ class RdPagedConfig(C.Structure):
 class RdPagedRows(C.Structure):
     _fields_ = [("n_rows", C.c_int32), ("n_groups", C.c_int32), ("group_start", C.c_void_p), ("max_group_rows", C.c_int32),
                 ("row_pos", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int32)]
+
+
+class RdPagedSessionConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("page_size", "n_pages", "window", "sinks")]
 
 
 class RdStats(C.Structure):
@@ -109,6 +113,8 @@ def lib():
         L.rd_profile_enable.argtypes = [vp, i32]
         L.rd_profile_read.argtypes = [vp, C.POINTER(RdProfile)]
         i64 = C.c_int64
+        L.rd_session_create_paged.argtypes = [vp, C.POINTER(RdSessionConfig), C.POINTER(RdPagedSessionConfig), vp, C.POINTER(vp)]
+        L.rd_session_release.argtypes = [vp, i32]
         L.rd_paged_create.argtypes = [C.POINTER(RdPagedConfig), vp, vp, C.POINTER(vp)]
         L.rd_paged_destroy.argtypes = [vp]
         L.rd_paged_destroy.restype = None
@@ -170,15 +176,21 @@ class Model:
 
 
 class Session:
-    """rd_session_create and the per-session calls."""
+    """rd_session_create and the per-session calls.  page_size > 0: rd_session_create_paged with pools of n_pages
+    pages (attn_window, attn_sinks: the positions a row attends)."""
 
     def __init__(self, model: Model, batch=1, max_context=1024, max_window=1, max_iters_per_pos=64,
                  max_new_tokens=64, keep_logits=False, temperature=0.0, seed=0, stream=None, eta=0.0, beta=0.0,
-                 top_p=0.0, latent_slots=0):
+                 top_p=0.0, latent_slots=0, page_size=0, n_pages=0, attn_window=0, attn_sinks=0):
         self.model = model
         self.sc = RdSessionConfig(batch, max_context, max_window, max_iters_per_pos, max_new_tokens,
                                   1 if keep_logits else 0, temperature, seed, eta, beta, top_p, latent_slots)
         self.handle = C.c_void_p()
+        if page_size or n_pages or attn_window or attn_sinks:
+            pc = RdPagedSessionConfig(page_size, n_pages, attn_window, attn_sinks)
+            _check(lib().rd_session_create_paged(model.handle, C.byref(self.sc), C.byref(pc), C.c_void_p(stream or 0),
+                                                 C.byref(self.handle)), "rd_session_create_paged")
+            return
         _check(lib().rd_session_create(model.handle, C.byref(self.sc), C.c_void_p(stream or 0),
                                        C.byref(self.handle)), "rd_session_create")
 
@@ -196,6 +208,10 @@ class Session:
     def prefill(self, seq, prompt, r):
         p = np.ascontiguousarray(prompt, dtype=np.int32)
         _check(lib().rd_prefill(self.handle, seq, p.ctypes.data, len(p), r), "rd_prefill")
+
+    def release(self, seq):
+        """Paged sessions: stops the sequence and returns its pages to the pool."""
+        _check(lib().rd_session_release(self.handle, seq), "rd_session_release")
 
     def prefill_sliced(self, seq, prompt, r):
         p = np.ascontiguousarray(prompt, dtype=np.int32)

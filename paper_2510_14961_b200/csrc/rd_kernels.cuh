@@ -963,8 +963,10 @@ struct SeqState {
 constexpr int RD_COUNTERS = 32;
 constexpr int RD_HIST_AT = 8, RD_HIST_BINS = 16;
 // layer_passes: layers a row goes through in this step (prelude + coda + inner_iters * core).
+// att_window, att_sinks: positions a row attends (0: all up to its own), for the counters of cache rows and keys.
 __global__ void advance_kernel(SeqState st, const float* __restrict__ delta, int B, int Wmax, int window,
-                               int inner_iters, float exit_threshold, int cap, int max_new, int layer_passes) {
+                               int inner_iters, float exit_threshold, int cap, int max_new, int layer_passes, int att_window,
+                               int att_sinks) {
     pdl_enter();
     const int b = blockIdx.x * blockDim.x + threadIdx.x;
     if (b >= B || st.done[b]) return;
@@ -984,8 +986,15 @@ __global__ void advance_kernel(SeqState st, const float* __restrict__ delta, int
     atomicAdd(&st.counters[2], (unsigned long long)w);
     // rows at positions f .. f+w-1: the cache rows 0 .. f+w-1 are read once for the whole window;
     // the row at position p attends p + 1 keys
-    atomicAdd(&st.counters[4], (unsigned long long)(f + w) * layer_passes);
-    atomicAdd(&st.counters[5], ((unsigned long long)w * (f + 1) + (unsigned long long)w * (w - 1) / 2) * layer_passes);
+    unsigned long long rows_read = f + w, keys = (unsigned long long)w * (f + 1) + (unsigned long long)w * (w - 1) / 2;
+    if (att_window > 0) {
+        const int lo = max(0, f - att_window + 1);        // oldest position a row of the wavefront sees beside the sinks
+        rows_read = (unsigned long long)(f + w - lo) + min(att_sinks, lo);
+        keys = 0;
+        for (int p = f; p < f + w; p++) keys += p < att_window ? p + 1 : att_window + min(att_sinks, p + 1 - att_window);
+    }
+    atomicAdd(&st.counters[4], rows_read * layer_passes);
+    atomicAdd(&st.counters[5], keys * layer_passes);
     int nc = st.n_committed[b];
     const int np = st.n_prompt[b];
     k = min(k, max_new - (nc - np));

@@ -300,6 +300,15 @@ struct rd_session {
     AttMaps att_maps[3];        // per block: boxes of 64 and 32 columns over the K and the V cache
     void *act_h = nullptr, *act_2h = nullptr, *act_i = nullptr, *q_t = nullptr;
     void *Kc[3] = {nullptr, nullptr, nullptr}, *Vc[3] = {nullptr, nullptr, nullptr};
+    // paged caches (rd_session_create_paged): one cache per block, all with the page numbers of pg_table [batch, pg_stride]
+    bool paged = false;
+    rd_paged_session_config pgc = {0, 0, 0, 0};
+    rd_paged* pg[3] = {nullptr, nullptr, nullptr};
+    int* pg_table = nullptr;
+    int pg_stride = 0;
+    std::vector<int> pg_free;                 // pages nobody holds
+    std::vector<std::vector<int>> pg_held;    // pages of every sequence, in order
+    PgBatch pg_rows = {};                     // the rows of the pass being enqueued
     TcAct t_act_h, t_act_2h, t_act_i;
     // host state
     std::vector<char> prefilled, wave_open;
@@ -314,6 +323,7 @@ struct rd_session {
     std::vector<cudaEvent_t> event_pool;
     uint64_t ctx_total = 0;   // host-side upper bound of sum over sequences of context length
     ~rd_session() {
+        for (rd_paged* c : pg) rd_paged_destroy(c);
         if (mirror) cudaFreeHost(mirror);
         for (int i = 0; i < 2; i++) {
             if (poll_mirror[i]) cudaFreeHost(poll_mirror[i]);
@@ -443,8 +453,8 @@ static int q_encode(CUtensorMap* map, const void* ptr, unsigned long long rows, 
     return r == CUDA_SUCCESS ? RD_OK : RD_E_CUDA;
 }
 
-extern "C" int rd_session_create(const rd_model* m, const rd_session_config* scp, void* cuda_stream,
-                                 rd_session** out) {
+static int session_create(const rd_model* m, const rd_session_config* scp, const rd_paged_session_config* pc, void* cuda_stream,
+                          rd_session** out) {
     if (!m || !scp || !out) return RD_E_INVALID_ARG;
     const rd_session_config& sc = *scp;
     if (sc.batch < 1 || sc.max_context < 2 || sc.max_window < 1 || sc.max_new_tokens < 0) return RD_E_INVALID_ARG;
@@ -455,6 +465,11 @@ extern "C" int rd_session_create(const rd_model* m, const rd_session_config* scp
     if (sc.temperature > 0.f && sc.top_p > 0.f && sc.top_p < 1.f && m->cfg.vocab > NUC_MAX_VOCAB) return RD_E_INVALID_ARG;
     if ((long long)sc.batch * sc.max_window > 4096) return RD_E_CAPACITY;
     if (sc.latent_slots < 0 || (long long)sc.latent_slots > (long long)sc.batch * sc.max_window) return RD_E_INVALID_ARG;
+    if (pc) {
+        if (pc->page_size < 16 || pc->page_size > 256 || (pc->page_size & (pc->page_size - 1)) || pc->n_pages < 1) return RD_E_INVALID_ARG;
+        if (pc->window < 0 || pc->sinks < 0) return RD_E_INVALID_ARG;
+        if (sc.latent_slots > 0 && sc.latent_slots < sc.batch * sc.max_window) return RD_E_INVALID_ARG;
+    }
     const bool pooled = sc.latent_slots > 0 && sc.latent_slots < sc.batch * sc.max_window;
     if (pooled && sc.batch > 1024) return RD_E_CAPACITY;        // one thread per sequence in the pool's bookkeeping kernel
     {
@@ -478,6 +493,11 @@ extern "C" int rd_session_create(const rd_model* m, const rd_session_config* scp
     s->tok_stride = sc.max_context + 1;
     s->seq_stride = (size_t)sc.max_context * h;
     s->head_stride = (size_t)sc.max_context * c.head_dim;
+    if (pc) {
+        s->paged = true;
+        s->pgc = *pc;
+        s->pg_stride = (sc.max_context + pc->page_size - 1) / pc->page_size;
+    }
     const size_t R = s->R, B = sc.batch;
     int rc = RD_OK;
     do {
@@ -519,7 +539,7 @@ extern "C" int rd_session_create(const rd_model* m, const rd_session_config* scp
         {
             cudaError_t eh = cudaSuccess;
             for (int i = 0; i < rd_session::PROMPT_STAGES && eh == cudaSuccess; i++) {
-                eh = cudaHostAlloc((void**)&s->prompt_stage[i], (size_t)s->tok_stride * sizeof(int), cudaHostAllocDefault);
+                eh = cudaHostAlloc((void**)&s->prompt_stage[i], (size_t)(s->tok_stride + s->pg_stride) * sizeof(int), cudaHostAllocDefault);
                 if (eh == cudaSuccess) eh = cudaEventCreateWithFlags(&s->prompt_ev[i], cudaEventDisableTiming);
             }
             if (eh != cudaSuccess) { rc = cuda_fail(eh, "prompt staging", __LINE__); break; }
@@ -550,7 +570,20 @@ extern "C" int rd_session_create(const rd_model* m, const rd_session_config* scp
         if ((rc = s->mem.get(&s->act_2h, Ra * 2 * h * es))) break;
         if ((rc = s->mem.get(&s->act_i, Ra * I * es))) break;
         if ((rc = s->mem.get(&s->q_t, R * h * es))) break;
-        for (int blk = 0; blk < 3 && !rc; blk++) {
+        if (s->paged) {
+            if ((rc = s->mem.get(&s->pg_table, B * s->pg_stride * sizeof(int)))) break;
+            for (int blk = 0; blk < 3 && !rc; blk++) {
+                if (n_layers_of(c, blk) == 0) continue;
+                const rd_paged_config g = {c.n_heads, c.n_heads, c.head_dim, c.dtype, pc->page_size, pc->n_pages, n_layers_of(c, blk),
+                                           sc.max_context, s->R, c.rope_base};
+                rc = rd_paged_create(&g, nullptr, nullptr, &s->pg[blk]);
+                if (rc == RD_OK) paged_set_status(s->pg[blk], s->status);
+            }
+            if (rc) break;
+            s->pg_held.resize(B);
+            for (int i = pc->n_pages; i-- > 0;) s->pg_free.push_back(i);       // page 0 is handed out first
+        }
+        for (int blk = 0; blk < 3 && !rc && !s->paged; blk++) {
             const size_t n = (size_t)n_layers_of(c, blk) * B * s->seq_stride * es;
             if ((rc = s->mem.get(&s->Kc[blk], n))) break;
             rc = s->mem.get(&s->Vc[blk], n);
@@ -573,7 +606,7 @@ extern "C" int rd_session_create(const rd_model* m, const rd_session_config* scp
         std::vector<int> ones(B, 1);
         if (e == cudaSuccess) e = cudaMemcpy(s->done, ones.data(), B * sizeof(int), cudaMemcpyHostToDevice);
         if (e != cudaSuccess) { rc = cuda_fail(e, "session init copies", __LINE__); break; }
-        if (c.dtype == RD_BF16 && (c.head_dim == 64 || c.head_dim == 96 || c.head_dim == 128)) {
+        if (!s->paged && c.dtype == RD_BF16 && (c.head_dim == 64 || c.head_dim == 96 || c.head_dim == 128)) {
             s->attn_path = 1;
             s->attn_capable = true;
             // TMA view of each cache: [layers * sequences * heads * max_context, head_dim], row coordinates stay below 2^31
@@ -624,6 +657,13 @@ extern "C" int rd_session_create(const rd_model* m, const rd_session_config* scp
     *out = s;
     return RD_OK;
 }
+extern "C" int rd_session_create(const rd_model* m, const rd_session_config* scp, void* cuda_stream, rd_session** out) {
+    return session_create(m, scp, nullptr, cuda_stream, out);
+}
+extern "C" int rd_session_create_paged(const rd_model* m, const rd_session_config* scp, const rd_paged_session_config* pc,
+                                       void* cuda_stream, rd_session** out) {
+    return pc ? session_create(m, scp, pc, cuda_stream, out) : RD_E_INVALID_ARG;
+}
 extern "C" void rd_session_destroy(rd_session* s) {
     if (!s) return;
     cudaStreamSynchronize(s->stream);
@@ -638,6 +678,7 @@ extern "C" int rd_set_gemm_path(rd_session* s, int32_t path) {
 
 extern "C" int rd_set_attention_path(rd_session* s, int32_t path) {
     if (!s || path < 0 || path > 3) return RD_E_INVALID_ARG;
+    if (s->paged) return RD_E_STATE;                                  // paged sessions have one attention path
     if (path >= 1 && !s->attn_capable) return RD_E_STATE;             // no tensor-core attention for this model
     if (path >= 2 && !s->att_maps_ok) return RD_E_STATE;
     if (path == 3 && !s->q_maps_ok) return RD_E_STATE;
@@ -829,15 +870,20 @@ template <typename T> struct Eng {
         const LayerW& L = s->m->layers[blk][l];
         const int h = c.hidden, I = c.mlp_inner;
         const size_t layer_off = (size_t)l * s->sc.batch * s->seq_stride;
-        T* Kc = (T*)s->Kc[blk] + layer_off;
-        T* Vc = (T*)s->Vc[blk] + layer_off;
+        T* Kc = s->paged ? nullptr : (T*)s->Kc[blk] + layer_off;
+        T* Vc = s->paged ? nullptr : (T*)s->Vc[blk] + layer_off;
         // x_in is materialised in s->x unless it already is a finished array
         const bool lazy = in.resid != nullptr || in.src.plain == nullptr;
         RD_TRY(norm<T>(s, in, lazy ? s->x : nullptr, L.g1, (T*)s->act_h, n_rows));
         const float* x_in = lazy ? s->x : in.src.plain;
         RowSource acc;
         RD_TRY(gemm(s, (T*)s->act_h, h, &s->t_act_h, (T*)L.wqkv, &L.t_qkv, h, 3 * h, n_rows, &acc));
-        if (n_rows >= 128) {
+        if (s->paged) {
+            const int bo = bracket_other(s);
+            RD_TRY(paged_append_sums(s->pg[blk], s->pg_rows, l, acc, s->q_t, s->stream, s->chained));
+            bracket_close(s, bo);
+            s->stats.kernel_launches++;
+        } else if (n_rows >= 128) {
             LAUNCH(s, (rope_kv_kernel<T, false>), dim3(n_rows, 16), 128, 0, acc, s->row_pos, s->row_seq, s->cos_t, s->sin_t, h, c.head_dim,
                    (T*)s->q_t, Kc, Vc, s->seq_stride, s->head_stride);
         } else {
@@ -846,7 +892,13 @@ template <typename T> struct Eng {
         }
         const int br = bracket_open(s, 1, s->ctx_total * 2 * h * sizeof(T));
         bool windowed = false;
-        if constexpr (sizeof(T) == 2) {
+        if (s->paged) {
+            int launches = 0;
+            RD_TRY(paged_attend(s->pg[blk], s->pg_rows, s->pg_rows.uniform, l, s->q_t, h, s->act_h, h, nullptr, s->pgc.window, s->pgc.sinks,
+                                0.f, s->stream, s->chained, &launches));
+            s->stats.kernel_launches += launches;
+            windowed = true;
+        } else if constexpr (sizeof(T) == 2) {
             if (s->attn_path >= 1 && s->grp_rows >= 1 && s->grp_rows <= ATT_QMAX) {
                 s->att_blk = blk; s->att_layer = l;
                 RD_TRY(attn_windowed(s, Kc, Vc, n_rows));
@@ -966,6 +1018,7 @@ template <typename T> struct Eng {
             }
         s->att_index = nullptr;
         s->att_groups = 0;
+        s->pg_rows = PgBatch{n, B, s->sc.max_window, nullptr, s->row_pos, s->pg_table, s->pg_stride};
         if (s->pooled) {
             LAUNCH(s, plan_rows_pool_kernel, 1, 1024, 0, s->n_committed, s->win_len, s->done, B, s->sc.max_window, n, s->pool,
                    s->row_pos, s->row_seq, s->grp_index, s->step_first, s->step_n);
@@ -991,7 +1044,7 @@ template <typename T> struct Eng {
                    s->sc.max_iters_per_pos, s->sc.max_new_tokens, c.n_prelude + c.n_coda + inner * c.n_core, s->pool);
         } else {
             LAUNCH(s, advance_kernel, (B + 63) / 64, 64, 0, st, s->delta, B, s->sc.max_window, window, inner, eps,
-                   s->sc.max_iters_per_pos, s->sc.max_new_tokens, c.n_prelude + c.n_coda + inner * c.n_core);
+                   s->sc.max_iters_per_pos, s->sc.max_new_tokens, c.n_prelude + c.n_coda + inner * c.n_core, s->pgc.window, s->pgc.sinks);
         }
         s->att_index = nullptr;
         s->att_groups = 0;
@@ -1033,6 +1086,7 @@ template <typename T> struct Eng {
         s->grp_rows = ATT_QMAX;
         s->att_index = nullptr;
         s->att_groups = 0;
+        s->pg_rows = PgBatch{nr, 1, nr, nullptr, s->row_pos, s->pg_table + (size_t)seq * s->pg_stride, s->pg_stride};
         s->ctx_max = c0 + nr;
         s->ctx_total = c0 + nr;
         s->grp_ctx.clear();
@@ -1063,6 +1117,11 @@ template <typename T> struct Eng {
         memcpy(s->prompt_stage[buf], prompt, (size_t)L * sizeof(int));
         CU(cudaMemcpyAsync(s->tokens + (size_t)seq * s->tok_stride, s->prompt_stage[buf], (size_t)L * sizeof(int),
                            cudaMemcpyHostToDevice, s->stream));
+        if (s->paged) {
+            int* row = s->prompt_stage[buf] + s->tok_stride;
+            for (int i = 0; i < s->pg_stride; i++) row[i] = i < (int)s->pg_held[seq].size() ? s->pg_held[seq][i] : -1;
+            CU(cudaMemcpyAsync(s->pg_table + (size_t)seq * s->pg_stride, row, (size_t)s->pg_stride * sizeof(int), cudaMemcpyHostToDevice, s->stream));
+        }
         CU(cudaEventRecord(s->prompt_ev[buf], s->stream));
         s->stage_next = (buf + 1) % rd_session::PROMPT_STAGES;
         return RD_OK;
@@ -1140,9 +1199,36 @@ static int prefill_args(const rd_session* s, int32_t seq, const int32_t* prompt,
     return RD_OK;
 }
 
+// Pages for `n` positions of sequence `seq` in the place of those it holds; nothing changes when the pool has too few.
+// (Passes enqueued before this call still read and write the old pages; whoever gets them is enqueued behind.)
+static int reserve_pages(rd_session* s, int seq, long long n) {
+    if (!s->paged) return RD_OK;
+    std::vector<int>& held = s->pg_held[seq];
+    const size_t need = (size_t)((n + s->pgc.page_size - 1) / s->pgc.page_size);
+    if (need > held.size() + s->pg_free.size()) return RD_E_CAPACITY;
+    while (held.size() > need) { s->pg_free.push_back(held.back()); held.pop_back(); }
+    while (held.size() < need) { held.push_back(s->pg_free.back()); s->pg_free.pop_back(); }
+    return RD_OK;
+}
+
+extern "C" int rd_session_release(rd_session* s, int32_t seq) {
+    if (!s || seq < 0 || seq >= s->sc.batch) return RD_E_INVALID_ARG;
+    if (!s->paged) return RD_E_STATE;
+    for (const rd_session::PrefillJob& j : s->jobs)
+        if (j.seq == seq) return RD_E_STATE;
+    if (s->prefilled[seq]) {
+        RD_TRY(Eng<float>::start_sequence(s, seq, 1, true));       // stopped: no in-flight rows
+        s->enqueue_epoch++;
+        s->prefilled[seq] = 0; s->wave_open[seq] = 0;
+        s->host_prompt_len[seq] = 0; s->host_steps[seq] = 0;
+    }
+    return reserve_pages(s, seq, 0);
+}
+
 extern "C" int rd_prefill(rd_session* s, int32_t seq, const int32_t* prompt, int32_t n_prompt, int32_t r) {
     RD_TRY(prefill_args(s, seq, prompt, n_prompt, r));
     if (!s->jobs.empty()) return RD_E_STATE;     // the prefill workspace belongs to the sliced jobs
+    RD_TRY(reserve_pages(s, seq, (long long)n_prompt + s->sc.max_new_tokens));
     const int rc = s->m->cfg.dtype == RD_BF16 ? Eng<bf16>::prefill(s, seq, prompt, n_prompt, r)
                                               : Eng<float>::prefill(s, seq, prompt, n_prompt, r);
     s->enqueue_epoch++;
@@ -1157,6 +1243,7 @@ extern "C" int rd_prefill_sliced(rd_session* s, int32_t seq, const int32_t* prom
     RD_TRY(prefill_args(s, seq, prompt, n_prompt, r));
     for (const rd_session::PrefillJob& j : s->jobs)
         if (j.seq == seq) return RD_E_STATE;
+    RD_TRY(reserve_pages(s, seq, (long long)n_prompt + s->sc.max_new_tokens));
     const int rc = s->m->cfg.dtype == RD_BF16 ? Eng<bf16>::prefill_sliced(s, seq, prompt, n_prompt, r)
                                               : Eng<float>::prefill_sliced(s, seq, prompt, n_prompt, r);
     s->enqueue_epoch++;
@@ -1340,6 +1427,7 @@ extern "C" int rd_debug_read_kv(rd_session* s, int32_t block, int32_t layer, int
     if (!s || !dst || block < 0 || block > 2 || (which != 0 && which != 1) || seq < 0 || seq >= s->sc.batch) return RD_E_INVALID_ARG;
     const rd_config& c = s->m->cfg;
     if (layer < 0 || layer >= n_layers_of(c, block) || pos0 < 0 || n < 0 || pos0 > s->sc.max_context || n > s->sc.max_context - pos0) return RD_E_INVALID_ARG;
+    if (s->paged && s->pg_held[seq].empty()) return RD_E_STATE;      // no pages: never prefilled, or released
     RD_TRY(rd_sync(s));
     if (n == 0) return RD_OK;
     const size_t off = ((size_t)layer * s->sc.batch + seq) * s->seq_stride;
@@ -1347,7 +1435,10 @@ extern "C" int rd_debug_read_kv(rd_session* s, int32_t block, int32_t layer, int
     const char* src = (const char*)(which ? s->Vc[block] : s->Kc[block]) + off * s->m->esz;
     float* tmp = nullptr;
     CU(cudaMalloc((void**)&tmp, cnt * 4));
-    if (c.dtype == RD_F32)
+    if (s->paged) {
+        const int rg = paged_gather(s->pg[block], s->pg_table + (size_t)seq * s->pg_stride, s->pg_stride, layer, which, pos0, n, tmp, s->stream);
+        if (rg) { cudaFree(tmp); return rg; }
+    } else if (c.dtype == RD_F32)
         kv_gather_kernel<float><<<256, 256, 0, s->stream>>>((const float*)src, s->head_stride, c.head_dim, c.hidden, pos0, n, tmp);
     else
         kv_gather_kernel<bf16><<<256, 256, 0, s->stream>>>((const bf16*)src, s->head_stride, c.head_dim, c.hidden, pos0, n, tmp);
@@ -1392,6 +1483,7 @@ extern "C" int rd_debug_read_kv_noalloc(rd_session* s, int32_t block, int32_t la
     if (!s || !dst || block < 0 || block > 2 || (which != 0 && which != 1) || seq < 0 || seq >= s->sc.batch) return RD_E_INVALID_ARG;
     const rd_config& c = s->m->cfg;
     if (layer < 0 || layer >= n_layers_of(c, block) || pos0 < 0 || n < 0 || pos0 > s->sc.max_context || n > s->sc.max_context - pos0) return RD_E_INVALID_ARG;
+    if (s->paged && s->pg_held[seq].empty()) return RD_E_STATE;      // no pages: never prefilled, or released
     const size_t cnt = (size_t)n * c.hidden;
     if (cnt > RD_KV_STAGE_ELEMS) {
         snprintf(g_cuda_err, sizeof g_cuda_err,
@@ -1409,7 +1501,9 @@ extern "C" int rd_debug_read_kv_noalloc(rd_session* s, int32_t block, int32_t la
     float* stage = nullptr;
     RD_TRY(kv_stage_address(dev, &stage));
     // every element of stage[0..cnt) is overwritten: nothing of an earlier call can show through
-    if (c.dtype == RD_F32)
+    if (s->paged)
+        RD_TRY(paged_gather(s->pg[block], s->pg_table + (size_t)seq * s->pg_stride, s->pg_stride, layer, which, pos0, n, stage, s->stream));
+    else if (c.dtype == RD_F32)
         kv_gather_kernel<float><<<256, 256, 0, s->stream>>>((const float*)src, s->head_stride, c.head_dim, c.hidden, pos0, n, stage);
     else
         kv_gather_kernel<bf16><<<256, 256, 0, s->stream>>>((const bf16*)src, s->head_stride, c.head_dim, c.hidden, pos0, n, stage);

@@ -193,7 +193,30 @@ static PgGeom geometry(const rd_paged* c, int layer) {
     const rd_paged_config& g = c->cfg;
     return PgGeom{g.n_heads, g.n_kv_heads, g.n_heads / g.n_kv_heads, g.head_dim, c->page_shift, g.n_pages, layer, g.max_context};
 }
-int* rd::paged_status(rd_paged* c) { return c->status; }
+void rd::paged_set_status(rd_paged* c, int* status) { c->status = c->wa.status = c->wb.status = status; }
+
+template <typename T>
+__global__ void __launch_bounds__(256) pg_gather_kernel(const T* __restrict__ pages, PgGeom ge, const int* __restrict__ table, int table_stride,
+                                                        int pos0, int n, float* __restrict__ dst) {
+    const int width = ge.n_kv * ge.D;
+    const long long total = (long long)n * width;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
+        const int pos = pos0 + (int)(i / width), m = (int)(i % width), pi = pos >> ge.page_shift;
+        const int pg = pi < table_stride ? table[pi] : -1;
+        float x = 0.f;
+        if (pg >= 0 && pg < ge.n_pages)
+            x = pg_to_f(pages[((((((size_t)ge.layer * ge.n_pages + pg) * ge.n_kv + m / ge.D) << ge.page_shift) + (pos & ((1 << ge.page_shift) - 1))) * ge.D) + m % ge.D]);
+        dst[i] = x;
+    }
+}
+int rd::paged_gather(rd_paged* c, const int* table_row, int table_stride, int layer, int which, int pos0, int n, float* dst, cudaStream_t st) {
+    const PgGeom ge = geometry(c, layer);
+    const void* pages = which ? c->v : c->k;
+    if (c->cfg.dtype == RD_BF16) pg_gather_kernel<bf16><<<256, 256, 0, st>>>((const bf16*)pages, ge, table_row, table_stride, pos0, n, dst);
+    else pg_gather_kernel<float><<<256, 256, 0, st>>>((const float*)pages, ge, table_row, table_stride, pos0, n, dst);
+    PCU(cudaGetLastError());
+    return RD_OK;
+}
 
 template <typename T, int VEC, typename Src>
 static int append_launch(rd_paged* c, const PgAppend& a, const Src& src, cudaStream_t st, bool chained) {

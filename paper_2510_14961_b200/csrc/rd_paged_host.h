@@ -13,6 +13,9 @@ int cuda_fail_at(cudaError_t e, const char* what, const char* file, int line);
 int paged_append_sums(rd_paged* c, const PgBatch& b, int layer, const RowSource& sums, void* q_out, cudaStream_t st, bool chained);
 int paged_attend(rd_paged* c, const PgBatch& b, int max_group_rows, int layer, const void* q, long long ldq, void* out, long long ldo,
                  float* lse, int window, int sinks, float scale, cudaStream_t st, bool chained, int* launches);
-// Device word the kernels of this cache raise.
-int* paged_status(rd_paged* c);
+// The kernels of this cache raise `status` (a device word) instead of the cache's own.
+void paged_set_status(rd_paged* c, int* status);
+// K (which 0) or V of positions pos0 .. pos0 + n - 1 of the sequence with this table row, as float32 [n, n_kv_heads * head_dim];
+// positions without a page read as zeros.
+int paged_gather(rd_paged* c, const int* table_row, int table_stride, int layer, int which, int pos0, int n, float* dst, cudaStream_t st);
 }  // namespace rd

@@ -448,3 +448,16 @@ def test_rows_the_device_finds_wrong_are_reported(dtype, D, n):
         assert (c.out[-1] == FILL).all() and (c.q_out[-1] == FILL).all()
         if call is attend:
             assert torch.equal(kp, c.kp)
+
+
+@pytest.mark.parametrize("H,G,D,page,window,sinks", [(8, 8, 64, 32, 0, 0), (8, 8, 128, 64, 100, 16), (16, 2, 96, 16, 70, 0)])
+def test_blocks_that_walk_over_many_items(H, G, D, page, window, sinks):
+    # more items than blocks, row tiles whose second half is empty between full ones, short and long ones next to each
+    # other, called again and again: every piece finds its barriers where the one before left them
+    c = Case(BF, H, G, D, page, [(257 + 9 * (i % 5) + (100 if i % 3 == 0 else 0), 5 + 37 * (i % 7)) for i in range(26)], seed=22, pad=2)
+    c.attend(window, sinks)
+    c.check_attend(window, sinks)
+    first = c.out.clone()
+    for _ in range(20):
+        c.attend(window, sinks)
+        assert torch.equal(first, c.out)
