@@ -355,6 +355,7 @@ class PagedRows:
         self.row_pos, self.table, self.group_start = row_pos, table, group_start
         self.c = RdPagedRows(row_pos.numel(), n_groups, _ptr(group_start), max_group_rows, _ptr(row_pos), _ptr(table),
                              table.stride(0) if n_groups > 1 else pages)
+        self.ref = C.byref(self.c)
 
 
 class PagedCache:
@@ -369,6 +370,7 @@ class PagedCache:
         self.cfg = RdPagedConfig(n_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, n_layers, max_context, max_rows, rope_base)
         self.handle = C.c_void_p()
         self.stream = stream
+        self._dtype = None                   # the cache's torch type, once a tensor of it has been seen
         for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
             if t is None:
                 continue
@@ -381,35 +383,41 @@ class PagedCache:
     def _typed(self, name, t):
         if not t.is_cuda or not str(t.dtype).endswith("bfloat16" if self.cfg.dtype == RD_BF16 else "float32"):
             raise ValueError(f"{name}: a device tensor of the cache's type")
+        self._dtype = t.dtype
 
     def _rows(self, name, t, n_rows, heads):
         """Address and row stride of [n_rows, heads, head_dim] (or [n_rows, heads * head_dim])."""
-        self._typed(name, t)
-        d = self.cfg.head_dim
-        if tuple(t.shape) not in ((n_rows, heads, d), (n_rows, heads * d)):
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, wanted ({n_rows}, {heads}, {d})")
-        inner = t.stride()[1:]
-        if t.numel() and (inner[-1] != 1 or (t.dim() == 3 and heads > 1 and inner[0] != d)):
+        if t.dtype is not self._dtype or not t.is_cuda:
+            self._typed(name, t)
+        d, shape, stride = self.cfg.head_dim, t.shape, t.stride()
+        if len(shape) == 3:
+            ok = shape[0] == n_rows and shape[1] == heads and shape[2] == d
+            flat = stride[2] == 1 and (heads == 1 or stride[1] == d)
+        else:
+            ok = len(shape) == 2 and shape[0] == n_rows and shape[1] == heads * d
+            flat = ok and stride[1] == 1
+        if not ok:
+            raise ValueError(f"{name}: shape {tuple(shape)}, wanted ({n_rows}, {heads}, {d})")
+        if not flat and n_rows:
             raise ValueError(f"{name}: heads and features must be contiguous")
-        return t.data_ptr(), (t.stride(0) if n_rows > 1 else heads * d)
-
-    def _stream(self, stream):
-        return C.c_void_p((self.stream if stream is None else stream) or 0)
+        return t.data_ptr(), (stride[0] if n_rows > 1 else heads * d)
 
     def append(self, rows, q, k, v, q_out, layer=0, stream=None):
         n, c = rows.c.n_rows, self.cfg
-        args = []
-        for name, t, h in (("q", q, c.n_heads), ("k", k, c.n_kv_heads), ("v", v, c.n_kv_heads), ("q_out", q_out, c.n_heads)):
-            args += self._rows(name, t, n, h)
-        _check(lib().rd_paged_append(self.handle, C.byref(rows.c), layer, *args, self._stream(stream)), "rd_paged_append")
+        h, g = c.n_heads, c.n_kv_heads
+        rc = lib().rd_paged_append(self.handle, rows.ref, layer, *self._rows("q", q, n, h), *self._rows("k", k, n, g),
+                                   *self._rows("v", v, n, g), *self._rows("q_out", q_out, n, h), self.stream if stream is None else stream)
+        if rc:
+            _check(rc, "rd_paged_append")
 
     def attend(self, rows, q, out, lse=None, layer=0, window=0, sinks=0, scale=0.0, stream=None):
-        n, c = rows.c.n_rows, self.cfg
-        qa, oa = self._rows("q", q, n, c.n_heads), self._rows("out", out, n, c.n_heads)
-        if lse is not None and (tuple(lse.shape) != (n, c.n_heads) or lse.element_size() != 4 or not lse.is_contiguous() or not lse.is_cuda):
-            raise ValueError(f"lse: contiguous float32 ({n}, {c.n_heads})")
-        _check(lib().rd_paged_attend(self.handle, C.byref(rows.c), layer, *qa, *oa, _ptr(lse), window, sinks, scale, self._stream(stream)),
-               "rd_paged_attend")
+        n, h = rows.c.n_rows, self.cfg.n_heads
+        if lse is not None and (lse.shape != (n, h) or lse.element_size() != 4 or not lse.is_contiguous() or not lse.is_cuda):
+            raise ValueError(f"lse: contiguous float32 ({n}, {h})")
+        rc = lib().rd_paged_attend(self.handle, rows.ref, layer, *self._rows("q", q, n, h), *self._rows("out", out, n, h),
+                                   None if lse is None else lse.data_ptr(), window, sinks, scale, self.stream if stream is None else stream)
+        if rc:
+            _check(rc, "rd_paged_attend")
 
     def pages(self):
         """Device addresses of the K and the V pages."""
@@ -418,7 +426,7 @@ class PagedCache:
         return k.value, v.value
 
     def sync(self, stream=None):
-        _check(lib().rd_paged_sync(self.handle, self._stream(stream)), "rd_paged_sync")
+        _check(lib().rd_paged_sync(self.handle, self.stream if stream is None else stream), "rd_paged_sync")
 
     def close(self):
         if self.handle:

@@ -221,10 +221,10 @@ int rd::paged_gather(rd_paged* c, const int* table_row, int table_stride, int la
 template <typename T, int VEC, typename Src>
 static int append_launch(rd_paged* c, const PgAppend& a, const Src& src, cudaStream_t st, bool chained) {
     const int items = (a.ge.n_heads + 2 * a.ge.n_kv) * (a.ge.D / VEC);
-    // a block per row takes four vectors per thread; few rows are cut finer so that they still reach most SMs
-    int parts = (items + 4 * PG_APPEND_THREADS - 1) / (4 * PG_APPEND_THREADS);
-    if (a.b.n_rows * parts < c->n_sms) parts = (items + PG_APPEND_THREADS - 1) / PG_APPEND_THREADS;
-    PCU(launch_chained(pg_append_kernel<T, VEC, Src>, dim3(a.b.n_rows, parts), dim3(PG_APPEND_THREADS), 0, st, chained, a, src));
+    const int parts = (items + 32 * PG_APPEND_U - 1) / (32 * PG_APPEND_U);       // warps of a row
+    const long long blocks = ((long long)a.b.n_rows * parts + PG_APPEND_WARPS - 1) / PG_APPEND_WARPS;
+    if (blocks > 0x7fffffffll || (long long)a.b.n_rows * parts > 0x7fffffffll) return RD_E_CAPACITY;
+    PCU(launch_chained(pg_append_kernel<T, VEC, Src>, dim3((unsigned)blocks), dim3(32 * PG_APPEND_WARPS), 0, st, chained, a, src, parts));
     return RD_OK;
 }
 // Features a thread moves at once: 16 bytes where head_dim is made of them, else four or two elements.

@@ -449,17 +449,19 @@ template <typename T, int VEC> struct alignas(sizeof(T) * VEC > 16 ? 16 : sizeof
 template <typename T> struct PgArrays {                   // three arrays of the cache's type (rd_paged_append)
     const T *q, *k, *v;
     long long ldq, ldk, ldv;
-    template <int VEC> __device__ __forceinline__ void load(int what, int r, int m, float* x) const {
+    template <int VEC> using Raw = PgVec<T, VEC>;         // (stays packed until it is used)
+    template <int VEC> __device__ __forceinline__ Raw<VEC> load(int what, int r, int m) const {
         const T* s = what == 0 ? q + (size_t)r * ldq : what == 1 ? k + (size_t)r * ldk : v + (size_t)r * ldv;
-        const PgVec<T, VEC> u = *reinterpret_cast<const PgVec<T, VEC>*>(s + m);
-#pragma unroll
-        for (int i = 0; i < VEC; i++) x[i] = pg_to_f(u.x[i]);
+        return *reinterpret_cast<const PgVec<T, VEC>*>(s + m);
     }
 };
 struct PgSums {                                           // sums of a QKV GEMM, [rows][q | k | v] (a session's layer)
     RowSource src;
     int nq, nk;                                           // features of q, of k
-    template <int VEC> __device__ __forceinline__ void load(int what, int r, int m, float* x) const {
+    template <int VEC> using Raw = PgVec<float, VEC>;
+    template <int VEC> __device__ __forceinline__ Raw<VEC> load(int what, int r, int m) const {
+        Raw<VEC> o;
+        float* x = o.x;
         const int at = m + (what == 0 ? 0 : what == 1 ? nq : nq + nk);
         if constexpr (VEC % 4 == 0) {
 #pragma unroll
@@ -471,6 +473,7 @@ struct PgSums {                                           // sums of a QKV GEMM,
 #pragma unroll
             for (int i = 0; i < VEC; i++) x[i] = row_source_load(src, r, at + i);
         }
+        return o;
     }
 };
 
@@ -483,80 +486,90 @@ struct PgAppend {
     void *k, *v;                 // pages
 };
 
-// Rotary embedding (adjacent pairs) of q and k at the row's position; q to q_out, k and v to the row's place
-// in its page.  Bound by memory: every value is read and written once (the angles come from L1 for all heads
-// but the first), VEC features (16 bytes of bf16) per thread and turn, four loads in flight.  Grid (rows, parts of a row).
-constexpr int PG_APPEND_THREADS = 256;
-template <typename T, int VEC, typename Src>
-__global__ void __launch_bounds__(PG_APPEND_THREADS) pg_append_kernel(const __grid_constant__ PgAppend p, const __grid_constant__ Src src) {
-    __shared__ int grp_s;
-    pdl_enter();
-    const int r = blockIdx.x, D = p.ge.D, per_head = D / VEC;
-    const int items = (p.ge.n_heads + 2 * p.ge.n_kv) * per_head, stride = gridDim.y * PG_APPEND_THREADS;
-    const int pos = p.b.row_pos[r];
-    if (pos < 0) return;
-    int grp;
-    if (p.b.group_start) {
-        // the row's group: one look at the group borders by all threads together
-        if (threadIdx.x == 0) grp_s = -1;
-        __syncthreads();
-        for (int i = threadIdx.x; i < p.b.n_groups; i += PG_APPEND_THREADS)
-            if (p.b.group_start[i] <= r && r < p.b.group_start[i + 1]) grp_s = i;
-        __syncthreads();
-        grp = grp_s;
-    } else {
-        grp = r / p.b.uniform;
-        if (grp >= p.b.n_groups) grp = -1;
+// Group of row r among ascending group borders, by a whole warp: 32 borders are looked at a time.  -1: behind the last group.
+__device__ __forceinline__ int pg_group_of(const PgBatch& b, int r) {
+    if (!b.group_start) {
+        const int g = r / b.uniform;
+        return g < b.n_groups ? g : -1;
     }
-    if (grp < 0) return;                                   // behind the last group
-    const long long row0 = pos < pg_pos_limit(p.b, p.ge) ? pg_row_of(p.b, p.ge, grp, 0, pos) : -1;
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = b.n_groups + 1;                        // the last border <= r lies in [lo, lo + n)
+    while (n > 128) {
+        const int step = (n + 31) / 32, i = lane * step;
+        const unsigned le = __ballot_sync(0xffffffffu, i < n && b.group_start[lo + i] <= r);
+        if (le == 0) return -1;
+        const int k = (31 - __clz(le)) * step;
+        lo += k;
+        n = min(step, n - k);
+    }
+    int count = 0;
+#pragma unroll
+    for (int j = 0; j < 4; j++) count += __popc(__ballot_sync(0xffffffffu, lane + 32 * j < n && b.group_start[lo + min(lane + 32 * j, n - 1)] <= r));
+    lo += count - 1;
+    return count > 0 && lo < b.n_groups ? lo : -1;
+}
+
+// Rotary embedding (adjacent pairs) of q and k at the row's position; q to q_out, k and v to the row's place
+// in its page.  Bound by memory: every value is read and written once.  A warp takes U x 32 vectors of VEC features
+// (16 bytes of bf16) of one row and asks for them before it looks for the row's group and page, whose loads depend on
+// one another; the angles come from L1 for all heads but the first.  Grid: warps of all rows, PG_APPEND_WARPS to a block.
+constexpr int PG_APPEND_WARPS = 8, PG_APPEND_U = 4;
+template <typename T, int VEC, typename Src>
+__global__ void __launch_bounds__(32 * PG_APPEND_WARPS) pg_append_kernel(const __grid_constant__ PgAppend p, const __grid_constant__ Src src, int parts) {
+    pdl_enter();
+    const int lane = threadIdx.x & 31, wid = blockIdx.x * PG_APPEND_WARPS + (threadIdx.x >> 5);
+    const int r = wid / parts, part = wid - r * parts;
+    if (r >= p.b.n_rows) return;
+    const int D = p.ge.D, per_head = D / VEC, items = (p.ge.n_heads + 2 * p.ge.n_kv) * per_head;
+    constexpr int U = PG_APPEND_U;
+    typename Src::template Raw<VEC> x[U];
+    const int first = part * U * 32 + lane, nq = p.ge.n_heads, nk = p.ge.n_kv;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int c = first + u * 32;
+        if (c < items) {
+            const int hd = c / per_head, what = hd < nq ? 0 : hd < nq + nk ? 1 : 2;
+            x[u] = src.template load<VEC>(what, r, (hd - (what == 0 ? 0 : what == 1 ? nq : nq + nk)) * D + (c - hd * per_head) * VEC);
+        }
+    }
+    const int pos = p.b.row_pos[r];
+    const int grp = pg_group_of(p.b, r);
+    if (pos < 0 || grp < 0) return;
+    const bool far = pos >= pg_pos_limit(p.b, p.ge);
+    // where a head's vectors are a divisor of a warp every turn of a lane has the same angles
+    const float2* cs = p.cs && !far ? p.cs + (size_t)pos * (D / 2) : nullptr;
+    const bool same = 32 % per_head == 0;
+    float2 a[VEC / 2];
+#pragma unroll
+    for (int i = 0; i < VEC / 2; i++) a[i] = cs && same ? cs[(lane % per_head) * (VEC / 2) + i] : make_float2(1.f, 0.f);
+    const long long row0 = far ? -1 : pg_row_of(p.b, p.ge, grp, 0, pos);
     if (row0 < 0) {
-        if (threadIdx.x == 0) atomicOr(p.status, pos < pg_pos_limit(p.b, p.ge) ? PG_ST_BAD_PAGE : PG_ST_BAD_ROW);
+        if (lane == 0) atomicOr(p.status, far ? PG_ST_BAD_ROW : PG_ST_BAD_PAGE);
         return;
     }
     T* kd = (T*)p.k + (size_t)row0 * D;
     T* vd = (T*)p.v + (size_t)row0 * D;
     const size_t head = (size_t)D << p.ge.page_shift;      // elements between a page's heads
     T* qd = (T*)p.q_out + (size_t)r * p.ldqo;
-    const float2* cs = p.cs ? p.cs + (size_t)pos * (D / 2) : nullptr;
-    constexpr int U = 4;
-    for (int c0 = blockIdx.y * PG_APPEND_THREADS + threadIdx.x; c0 < items; c0 += U * stride) {
-        float x[U][VEC];
-        int hd[U], e[U];
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int c = c0 + u * stride;
-            hd[u] = -1;
-            if (c < items) {
-                hd[u] = c / per_head;
-                e[u] = (c - hd[u] * per_head) * VEC;
-                const int what = hd[u] < p.ge.n_heads ? 0 : hd[u] < p.ge.n_heads + p.ge.n_kv ? 1 : 2;
-                src.template load<VEC>(what, r, (hd[u] - (what == 0 ? 0 : what == 1 ? p.ge.n_heads : p.ge.n_heads + p.ge.n_kv)) * D + e[u], x[u]);
-            }
+    for (int u = 0; u < U; u++) {
+        const int c = first + u * 32;
+        if (c >= items) break;
+        const int hd = c / per_head, e = (c - hd * per_head) * VEC;
+        if (cs && !same) {
+#pragma unroll
+            for (int i = 0; i < VEC / 2; i++) a[i] = cs[e / 2 + i];
         }
+        T* dst = hd < nq ? qd + (size_t)hd * D + e : hd < nq + nk ? kd + (size_t)(hd - nq) * head + e : vd + (size_t)(hd - nq - nk) * head + e;
+        const bool turn = cs && hd < nq + nk;
+        PgVec<T, VEC> o;
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            if (hd[u] < 0) continue;
-            T* dst;
-            bool turn = cs != nullptr;
-            if (hd[u] < p.ge.n_heads) dst = qd + (size_t)hd[u] * D + e[u];
-            else if (hd[u] < p.ge.n_heads + p.ge.n_kv) dst = kd + (size_t)(hd[u] - p.ge.n_heads) * head + e[u];
-            else { dst = vd + (size_t)(hd[u] - p.ge.n_heads - p.ge.n_kv) * head + e[u]; turn = false; }
-            PgVec<T, VEC> o;
-#pragma unroll
-            for (int i = 0; i < VEC; i += 2) {
-                float a = x[u][i], b = x[u][i + 1];
-                if (turn) {
-                    const float2 t = cs[(e[u] + i) / 2];
-                    const float y = a * t.x - b * t.y;
-                    b = a * t.y + b * t.x;
-                    a = y;
-                }
-                o.x[i] = pg_from_f<T>(a);
-                o.x[i + 1] = pg_from_f<T>(b);
-            }
-            *reinterpret_cast<PgVec<T, VEC>*>(dst) = o;
+        for (int i = 0; i < VEC; i += 2) {
+            const float s = pg_to_f(x[u].x[i]), t = pg_to_f(x[u].x[i + 1]);
+            o.x[i] = pg_from_f<T>(turn ? s * a[i / 2].x - t * a[i / 2].y : s);
+            o.x[i + 1] = pg_from_f<T>(turn ? s * a[i / 2].y + t * a[i / 2].x : t);
         }
+        *reinterpret_cast<PgVec<T, VEC>*>(dst) = o;
     }
 }
 
