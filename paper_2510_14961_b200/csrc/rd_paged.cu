@@ -153,7 +153,7 @@ extern "C" int rd_paged_create(const rd_paged_config* cfg, void* k_pages, void* 
     if (g.dtype != RD_F32 && g.dtype != RD_BF16) return RD_E_INVALID_ARG;
     if (g.page_size < 16 || g.page_size > 256 || (g.page_size & (g.page_size - 1))) return RD_E_INVALID_ARG;
     if (g.n_pages < 1 || g.n_layers < 1 || g.max_context < 1 || g.max_rows < 0 || !(g.rope_base >= 0.f) || !isfinite(g.rope_base)) return RD_E_INVALID_ARG;
-    if (g.n_heads > 65536 || ((uintptr_t)k_pages & 15) || ((uintptr_t)v_pages & 15)) return RD_E_INVALID_ARG;
+    if (g.n_heads > 65536 || g.n_kv_heads > 65536 || ((uintptr_t)k_pages & 15) || ((uintptr_t)v_pages & 15)) return RD_E_INVALID_ARG;
     // TMA names pool rows by 32-bit coordinates
     const double rows = (double)g.n_layers * g.n_pages * g.n_kv_heads * g.page_size;
     if (rows > 2147483647.0 - 512.0) return RD_E_CAPACITY;
@@ -220,11 +220,11 @@ int rd::paged_gather(rd_paged* c, const int* table_row, int table_stride, int la
 
 template <typename T, int VEC, typename Src>
 static int append_launch(rd_paged* c, const PgAppend& a, const Src& src, cudaStream_t st, bool chained) {
-    const int items = (a.ge.n_heads + 2 * a.ge.n_kv) * (a.ge.D / VEC);
-    const int parts = (items + 32 * PG_APPEND_U - 1) / (32 * PG_APPEND_U);       // warps of a row
-    const long long blocks = ((long long)a.b.n_rows * parts + PG_APPEND_WARPS - 1) / PG_APPEND_WARPS;
-    if (blocks > 0x7fffffffll || (long long)a.b.n_rows * parts > 0x7fffffffll) return RD_E_CAPACITY;
-    PCU(launch_chained(pg_append_kernel<T, VEC, Src>, dim3((unsigned)blocks), dim3(32 * PG_APPEND_WARPS), 0, st, chained, a, src, parts));
+    const int per_head = a.ge.D / VEC, items = (a.ge.n_heads + 2 * a.ge.n_kv) * per_head;
+    const int parts = (items + 32 * PG_APPEND_U - 1) / (32 * PG_APPEND_U), warps = std::min(parts, PG_APPEND_WARPS);       // warps of a row, of a block
+    PgAppend b = a;
+    b.head_magic = (unsigned)((0x100000000ull + per_head - 1) / per_head);
+    PCU(launch_chained(pg_append_kernel<T, VEC, Src>, dim3(a.b.n_rows, (parts + warps - 1) / warps), dim3(32 * warps), 0, st, chained, b, src));
     return RD_OK;
 }
 // Features a thread moves at once: 16 bytes where head_dim is made of them, else four or two elements.

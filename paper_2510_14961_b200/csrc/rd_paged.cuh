@@ -445,6 +445,18 @@ template <> __device__ __forceinline__ __nv_bfloat16 pg_from_f<__nv_bfloat16>(fl
 // VEC features at once, as wide as their bytes allow.
 template <typename T, int VEC> struct alignas(sizeof(T) * VEC > 16 ? 16 : sizeof(T) * VEC) PgVec { T x[VEC]; };
 
+// Two neighbouring features of a vector as floats, and back (bf16: one word; its high halves are the floats' own bits).
+__device__ __forceinline__ void pg_pair(const float* x, float* a, float* b) { *a = x[0]; *b = x[1]; }
+__device__ __forceinline__ void pg_pair(const __nv_bfloat16* x, float* a, float* b) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(x);
+    *a = __uint_as_float(w << 16); *b = __uint_as_float(w & 0xffff0000u);
+}
+__device__ __forceinline__ void pg_set_pair(float* x, float a, float b) { x[0] = a; x[1] = b; }
+__device__ __forceinline__ void pg_set_pair(__nv_bfloat16* x, float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    *reinterpret_cast<uint32_t*>(x) = *reinterpret_cast<const uint32_t*>(&v);
+}
+
 // Sources of the new rows: q of feature m (0 .. n_heads D - 1), k and v of feature m (0 .. n_kv D - 1).
 template <typename T> struct PgArrays {                   // three arrays of the cache's type (rd_paged_append)
     const T *q, *k, *v;
@@ -484,6 +496,7 @@ struct PgAppend {
     const float2* cs;            // rotary table, or null: q and k are stored as they come
     void* q_out; long long ldqo;
     void *k, *v;                 // pages
+    unsigned head_magic;         // 2^32 / (vectors of a head), rounded up: vector -> head by one multiplication (vectors of a row < 2^26)
 };
 
 // Group of row r among ascending group borders, by a whole warp: 32 borders are looked at a time.  -1: behind the last group.
@@ -512,14 +525,12 @@ __device__ __forceinline__ int pg_group_of(const PgBatch& b, int r) {
 // Rotary embedding (adjacent pairs) of q and k at the row's position; q to q_out, k and v to the row's place
 // in its page.  Bound by memory: every value is read and written once.  A warp takes U x 32 vectors of VEC features
 // (16 bytes of bf16) of one row and asks for them before it looks for the row's group and page, whose loads depend on
-// one another; the angles come from L1 for all heads but the first.  Grid: warps of all rows, PG_APPEND_WARPS to a block.
+// one another; the angles come from L1 for all heads but the first.  Grid (rows, parts of a row), up to PG_APPEND_WARPS warps.
 constexpr int PG_APPEND_WARPS = 8, PG_APPEND_U = 4;
 template <typename T, int VEC, typename Src>
-__global__ void __launch_bounds__(32 * PG_APPEND_WARPS) pg_append_kernel(const __grid_constant__ PgAppend p, const __grid_constant__ Src src, int parts) {
+__global__ void __launch_bounds__(32 * PG_APPEND_WARPS) pg_append_kernel(const __grid_constant__ PgAppend p, const __grid_constant__ Src src) {
     pdl_enter();
-    const int lane = threadIdx.x & 31, wid = blockIdx.x * PG_APPEND_WARPS + (threadIdx.x >> 5);
-    const int r = wid / parts, part = wid - r * parts;
-    if (r >= p.b.n_rows) return;
+    const int lane = threadIdx.x & 31, r = blockIdx.x, part = blockIdx.y * (blockDim.x >> 5) + (threadIdx.x >> 5);
     const int D = p.ge.D, per_head = D / VEC, items = (p.ge.n_heads + 2 * p.ge.n_kv) * per_head;
     constexpr int U = PG_APPEND_U;
     typename Src::template Raw<VEC> x[U];
@@ -528,7 +539,7 @@ __global__ void __launch_bounds__(32 * PG_APPEND_WARPS) pg_append_kernel(const _
     for (int u = 0; u < U; u++) {
         const int c = first + u * 32;
         if (c < items) {
-            const int hd = c / per_head, what = hd < nq ? 0 : hd < nq + nk ? 1 : 2;
+            const int hd = per_head == 1 ? c : (int)__umulhi((unsigned)c, p.head_magic), what = hd < nq ? 0 : hd < nq + nk ? 1 : 2;
             x[u] = src.template load<VEC>(what, r, (hd - (what == 0 ? 0 : what == 1 ? nq : nq + nk)) * D + (c - hd * per_head) * VEC);
         }
     }
@@ -538,10 +549,10 @@ __global__ void __launch_bounds__(32 * PG_APPEND_WARPS) pg_append_kernel(const _
     const bool far = pos >= pg_pos_limit(p.b, p.ge);
     // where a head's vectors are a divisor of a warp every turn of a lane has the same angles
     const float2* cs = p.cs && !far ? p.cs + (size_t)pos * (D / 2) : nullptr;
-    const bool same = 32 % per_head == 0;
+    const bool same = (per_head & (per_head - 1)) == 0 && per_head <= 32;
     float2 a[VEC / 2];
 #pragma unroll
-    for (int i = 0; i < VEC / 2; i++) a[i] = cs && same ? cs[(lane % per_head) * (VEC / 2) + i] : make_float2(1.f, 0.f);
+    for (int i = 0; i < VEC / 2; i++) a[i] = cs && same ? cs[(lane & (per_head - 1)) * (VEC / 2) + i] : make_float2(1.f, 0.f);
     const long long row0 = far ? -1 : pg_row_of(p.b, p.ge, grp, 0, pos);
     if (row0 < 0) {
         if (lane == 0) atomicOr(p.status, far ? PG_ST_BAD_ROW : PG_ST_BAD_PAGE);
@@ -555,7 +566,7 @@ __global__ void __launch_bounds__(32 * PG_APPEND_WARPS) pg_append_kernel(const _
     for (int u = 0; u < U; u++) {
         const int c = first + u * 32;
         if (c >= items) break;
-        const int hd = c / per_head, e = (c - hd * per_head) * VEC;
+        const int hd = per_head == 1 ? c : (int)__umulhi((unsigned)c, p.head_magic), e = (c - hd * per_head) * VEC;
         if (cs && !same) {
 #pragma unroll
             for (int i = 0; i < VEC / 2; i++) a[i] = cs[e / 2 + i];
@@ -565,9 +576,9 @@ __global__ void __launch_bounds__(32 * PG_APPEND_WARPS) pg_append_kernel(const _
         PgVec<T, VEC> o;
 #pragma unroll
         for (int i = 0; i < VEC; i += 2) {
-            const float s = pg_to_f(x[u].x[i]), t = pg_to_f(x[u].x[i + 1]);
-            o.x[i] = pg_from_f<T>(turn ? s * a[i / 2].x - t * a[i / 2].y : s);
-            o.x[i + 1] = pg_from_f<T>(turn ? s * a[i / 2].y + t * a[i / 2].x : t);
+            float s, t;
+            pg_pair(x[u].x + i, &s, &t);
+            pg_set_pair(o.x + i, turn ? s * a[i / 2].x - t * a[i / 2].y : s, turn ? s * a[i / 2].y + t * a[i / 2].x : t);
         }
         *reinterpret_cast<PgVec<T, VEC>*>(dst) = o;
     }

@@ -20,6 +20,8 @@ APPEND = [
     (BF, 3, 3, 12, 256, [(9, 250)], dict(ld_extra=4)),    # four features at a time
     (BF, 2, 2, 128, 128, [(300, 0), [7, 3, -1, 5]], dict(pad=2, n_layers=3, layer=1)),
     (F4, 8, 2, 32, 64, [(3, 60)], dict(rope_base=0.0)),
+    (BF, 5, 5, 8, 16, [(6, 3)], {}), (F4, 3, 1, 4, 16, [(4, 14)], {}), (F4, 3, 3, 2, 16, [(4, 14)], {}),       # a head is one vector
+    (BF, 48, 16, 128, 16, [(3, 2)], {}), (BF, 64, 64, 96, 32, [(2, 31)], {}),                                 # several parts of a row
     (BF, 2, 1, 64, 16, [(2, 130000)], {}),                # far positions: the angle keeps its fraction
 ]
 
