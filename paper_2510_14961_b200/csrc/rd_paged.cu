@@ -131,7 +131,7 @@ static int create_impl(rd_paged* c, void* k, void* v) {
     c->cap_b = (int)std::min<long long>(PG_MAX_GROUPS + packed / 64 + 1, 1 << 28);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-    const size_t o_st = take(256), o_ca = take((size_t)nb * 4), o_cb = take((size_t)nb * 8 * 4);     // (at most two blocks per SM)
+    const size_t o_st = take(256), o_ca = take((size_t)nb * 4), o_cb = take((size_t)nb * 4), o_cut = take((size_t)nb * sizeof(PgPiece));     // (at most two blocks per SM)
     const size_t o_ra = take((size_t)c->cap_a * sizeof(PgRecord)), o_rb = take((size_t)c->cap_b * sizeof(PgRecord));
     // the kernels on tensor cores run one block per SM, the others up to two
     const size_t slots = 2 * (size_t)(c->tensor ? c->n_sms : nb);
@@ -139,8 +139,8 @@ static int create_impl(rd_paged* c, void* k, void* v) {
     PCU(cudaMalloc((void**)&c->work, at));
     PCU(cudaMemset(c->work, 0, o_ra));
     c->status = (int*)(c->work + o_st);
-    c->wa = PgWork{(PgRecord*)(c->work + o_ra), c->status + 1, (int*)(c->work + o_ca), (float*)(c->work + o_pa), c->status};
-    c->wb = PgWork{(PgRecord*)(c->work + o_rb), c->status + 2, (int*)(c->work + o_cb), (float*)(c->work + o_pb), c->status};
+    c->wa = PgWork{(PgRecord*)(c->work + o_ra), c->status + 1, (int*)(c->work + o_ca), (float*)(c->work + o_pa), nullptr, c->status};
+    c->wb = PgWork{(PgRecord*)(c->work + o_rb), c->status + 2, (int*)(c->work + o_cb), (float*)(c->work + o_pb), (PgPiece*)(c->work + o_cut), c->status};
     PCU(cudaDeviceSynchronize());
     return RD_OK;
 }
@@ -268,7 +268,12 @@ template <int D> static int attend_few_tensor(rd_paged* c, const PgAttend& a, in
     return attend_launch<PGM_KT>(c, a, false, {64, PGM_THREADS, 1}, true, pg_attend_mma_kernel<D, 4>, PgmCfg<D, 4>::SMEM, st, chained, launches, c->maps_few);
 }
 template <int D> static int attend_many_tensor(rd_paged* c, const PgAttend& a, cudaStream_t st, bool chained, int* launches) {
-    return attend_launch<PGT_KT>(c, a, true, {PGT_M, PGT_THREADS, 1}, false, pg_attend_tc_kernel<D>, PgtCfg<D>::SMEM, st, chained, launches, c->maps_many);
+    PTRY(attend_launch<PGT_KT>(c, a, true, {PGT_M, PGT_THREADS, 1}, false, pg_attend_tc_kernel<D>, PgtCfg<D>::SMEM, st, chained, launches, c->maps_many));
+    PgAttend j = a;
+    j.w = c->wb;
+    PCU(launch_chained(pg_join_tc_kernel<D>, dim3(c->n_sms, PGT_M / 32), dim3(256), 0, st, chained, j));
+    if (launches) ++*launches;
+    return RD_OK;
 }
 template <typename T, int DP> static int attend_simt(rd_paged* c, const PgAttend& a, bool many, cudaStream_t st, bool chained, int* launches) {
     if (!many) return attend_launch<PGS_KT>(c, a, false, {PGS_FEW, PGS_THREADS, 1}, true, pg_attend_few_kernel<T, DP>, PgsFew<T, DP>::SMEM, st, chained, launches);

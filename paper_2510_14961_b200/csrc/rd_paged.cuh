@@ -48,11 +48,17 @@ struct PgRecord {                // one row tile
     int grp, a, n, rt;           // group, its first row, its rows, number of the tile in the group
     int pmin, pmax, nt, pad;     // smallest and largest position of its rows, key tiles
 };
+// One piece of an item: key tiles [i0, i1) of (row tile, kv head).
+struct PgPiece {
+    int grp, a, n, rt, head, i0, i1, nt, pmin, pmax;
+    int c_first, c_last;         // blocks whose shares hold the item; equal: the piece is the whole item
+};
 struct PgWork {                  // one launch's share of the workspace
     PgRecord* rec;               // external plan: records, with their number in *n_rec
     int* n_rec;
     int* counter;                // [blocks] shares of the cut item that starts in a block which have arrived; 0 between launches
     float* part;                 // [2 * blocks][M][D + 2]
+    PgPiece* cut;                // [blocks] the cut item that starts in a block (i1 < 0: none), for a joining kernel
     int* status;
 };
 struct PgAttend {
@@ -300,11 +306,6 @@ __device__ void pg_plan_share(const PgAttend& p, int M, PgPlanSmem<CAP>& sm) {
     __syncthreads();
 }
 
-// One piece of an item: key tiles [i0, i1) of (row tile, kv head).
-struct PgPiece {
-    int grp, a, n, rt, head, i0, i1, nt, pmin, pmax;
-    int c_first, c_last;         // blocks whose shares hold the item; equal: the piece is the whole item
-};
 // Walks a share piece by piece; every caller that walks (several warps may) sees the same pieces.
 struct PgWalk {
     long long u, u1, per;

@@ -154,6 +154,7 @@ pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ 
     }
     if (warp == 9) tmem_alloc(&tmem_slot, 512);
     pdl_enter();
+    if (tid == 0) p.w.cut[blockIdx.x].i1 = -1;
     tc_fence_before();
     pg_plan_share<PGT_THREADS, PGT_KT>(p, M, plan);
     tc_fence_after();
@@ -572,48 +573,7 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                 if (real && p.lse) p.lse[(size_t)row * p.ge.n_heads + hd] = (m + log2f(l)) * 0.6931471805599453f;
             } else {
                 if (real) *reinterpret_cast<float2*>(slot + (size_t)M * D + 2 * rm) = make_float2(m, l);
-                // a warp's 32 rows are joined by the warp that arrives last with them; no block waits for another
-                __threadfence();
-                __syncwarp();
-                int last = 0;
-                if (lane == 0) {
-                    int* ctr = p.w.counter + pc.c_first * 8 + warp;
-                    last = atomicAdd(ctr, 1) == pc.c_last - pc.c_first;
-                    if (last) atomicExch(ctr, 0);
-                    __threadfence();
-                }
-                last = __shfl_sync(0xffffffffu, last, 0);
-                if (last) {
-                    __threadfence();
-                    const int nseg = pc.c_last - pc.c_first + 1;
-                    if (real) {
-                        float mm = -INFINITY, den = 0.f;
-                        for (int s = 0; s < nseg; s++) mm = fmaxf(mm, __ldcg(pg_slot(p.w, pc.c_first + s, pc.c_first, M, D) + (size_t)M * D + 2 * rm));
-                        for (int s = 0; s < nseg; s++) {
-                            const float2 ml = __ldcg(reinterpret_cast<const float2*>(pg_slot(p.w, pc.c_first + s, pc.c_first, M, D) + (size_t)M * D + 2 * rm));
-                            den = fmaf(ml.y, ml.x == -INFINITY ? 0.f : exp2f(ml.x - mm), den);
-                        }
-                        const float iv = 1.0f / den;
-#pragma unroll 2
-                        for (int c = 0; c < D; c += 8) {
-                            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-                            for (int s = 0; s < nseg; s++) {
-                                const float* sl = pg_slot(p.w, pc.c_first + s, pc.c_first, M, D);
-                                const float ms = __ldcg(sl + (size_t)M * D + 2 * rm), f = ms == -INFINITY ? 0.f : exp2f(ms - mm);
-                                const float4 x = __ldcg(reinterpret_cast<const float4*>(sl + ((size_t)(c / 4) * M + rm) * 4));
-                                const float4 y = __ldcg(reinterpret_cast<const float4*>(sl + ((size_t)(c / 4 + 1) * M + rm) * 4));
-                                acc[0] = fmaf(x.x, f, acc[0]); acc[1] = fmaf(x.y, f, acc[1]); acc[2] = fmaf(x.z, f, acc[2]); acc[3] = fmaf(x.w, f, acc[3]);
-                                acc[4] = fmaf(y.x, f, acc[4]); acc[5] = fmaf(y.y, f, acc[5]); acc[6] = fmaf(y.z, f, acc[6]); acc[7] = fmaf(y.w, f, acc[7]);
-                            }
-                            uint32_t x[4];
-#pragma unroll
-                            for (int q = 0; q < 4; q++) x[q] = pack_bf16(acc[2 * q] * iv, acc[2 * q + 1] * iv);
-                            *reinterpret_cast<uint4*>(dst + c) = make_uint4(x[0], x[1], x[2], x[3]);
-                        }
-                        if (p.lse) p.lse[(size_t)row * p.ge.n_heads + hd] = (mm + log2f(den)) * 0.6931471805599453f;
-                    }
-                }
+                if (tid == 0 && pc.c_first == (int)blockIdx.x) p.w.cut[blockIdx.x] = pc;      // for the joining kernel
             }
             tc_fence_before();
             __syncwarp();
@@ -628,6 +588,48 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
+}
+
+// Joins the items that were cut between blocks, all over the GPU (a block that joined the parts of its item by itself
+// read up to 18 parts of 133 KB through one SM: 64 rows behind 8,000 positions took 84 us).  Grid (blocks of the
+// attention kernel, 8 runs of 32 rows); a thread takes D / 8 features of a row, parts in key order.
+template <int D>
+__global__ void __launch_bounds__(256) pg_join_tc_kernel(const __grid_constant__ PgAttend p) {
+    constexpr int M = PGT_M, E = D / 8;
+    pdl_enter();
+    const PgPiece pc = p.w.cut[blockIdx.x];
+    const int rows = pc.i1 < 0 ? 0 : (int)min((unsigned)M, (unsigned)pc.n * p.ge.g - (unsigned)pc.rt * M);
+    const int r = blockIdx.y * 32 + (threadIdx.x & 31), e0 = (threadIdx.x >> 5) * E;
+    if (r >= rows) return;
+    const unsigned pk = (unsigned)pc.rt * M + r, of = pk / (unsigned)p.ge.g;
+    const int row = pc.a + (int)of, hd = pc.head * p.ge.g + (int)(pk - of * p.ge.g), pos = p.b.row_pos[row];
+    if (pos < 0 || pos >= pg_pos_limit(p.b, p.ge)) return;
+    const int ns = pc.c_last - pc.c_first + 1;
+    float mx = -INFINITY, den = 0.f, acc[E];
+#pragma unroll 4
+    for (int s = 0; s < ns; s++) mx = fmaxf(mx, __ldcg(pg_slot(p.w, pc.c_first + s, pc.c_first, M, D) + (size_t)M * D + 2 * r));
+#pragma unroll
+    for (int e = 0; e < E; e++) acc[e] = 0.f;
+#pragma unroll 2
+    for (int s = 0; s < ns; s++) {
+        const float* sl = pg_slot(p.w, pc.c_first + s, pc.c_first, M, D);
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(sl + (size_t)M * D + 2 * r));
+        float4 x[E / 4];
+#pragma unroll
+        for (int e = 0; e < E / 4; e++) x[e] = __ldcg(reinterpret_cast<const float4*>(sl + ((size_t)(e0 / 4 + e) * M + r) * 4));
+        const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mx);
+#pragma unroll
+        for (int e = 0; e < E / 4; e++) {
+            acc[4 * e] = fmaf(x[e].x, f, acc[4 * e]); acc[4 * e + 1] = fmaf(x[e].y, f, acc[4 * e + 1]);
+            acc[4 * e + 2] = fmaf(x[e].z, f, acc[4 * e + 2]); acc[4 * e + 3] = fmaf(x[e].w, f, acc[4 * e + 3]);
+        }
+        den = fmaf(ml.y, f, den);
+    }
+    const float inv = 1.0f / den;
+    __nv_bfloat16* dst = (__nv_bfloat16*)p.out + (size_t)row * p.ldo + (size_t)hd * D + e0;
+#pragma unroll
+    for (int e = 0; e < E; e += 4) pg_store4(dst + e, acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv);
+    if (p.lse && e0 == 0) p.lse[(size_t)row * p.ge.n_heads + hd] = (mx + log2f(den)) * 0.6931471805599453f;
 }
 
 }  // namespace rd
