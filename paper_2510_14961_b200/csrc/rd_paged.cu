@@ -288,16 +288,16 @@ template <typename T> static int attend_simt_d(rd_paged* c, const PgAttend& a, b
 static int attend_part(rd_paged* c, PgAttend a, bool many, int m, cudaStream_t st, bool chained, int* launches) {
     if (c->tensor) {
         a.min_share = many ? 1 : 8;
-        a.item_cost = many ? 4 : 2;
-        a.whole_units = many ? 8 : 32;
+        a.item_cost = many ? 4 : 12;
+        a.whole_units = many ? 8 : 40;
         if (many) return a.ge.D == 64 ? attend_many_tensor<64>(c, a, st, chained, launches) : a.ge.D == 96 ? attend_many_tensor<96>(c, a, st, chained, launches)
                                                                                                 : attend_many_tensor<128>(c, a, st, chained, launches);
         return a.ge.D == 64 ? attend_few_tensor<64>(c, a, m, st, chained, launches) : a.ge.D == 96 ? attend_few_tensor<96>(c, a, m, st, chained, launches)
                                                                                        : attend_few_tensor<128>(c, a, m, st, chained, launches);
     }
     a.min_share = 1;
-    a.item_cost = 1;
-    a.whole_units = 4;
+    a.item_cost = 2;
+    a.whole_units = 2;
     return c->cfg.dtype == RD_BF16 ? attend_simt_d<bf16>(c, a, many, st, chained, launches) : attend_simt_d<float>(c, a, many, st, chained, launches);
 }
 

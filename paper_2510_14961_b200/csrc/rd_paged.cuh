@@ -426,6 +426,27 @@ __device__ __forceinline__ void pg_join_any(const PgAttend& p, const PgPiece& pc
     else pg_join<T, 1>(p, pc, M, D, tid, threads);
 }
 
+// What feature e of the row at position `pos` gets from the non-finite elements of V among the keys it sees in
+// key tiles [i0, i1) that were multiplied without them (partial tiles).  A weight is positive, so an infinity
+// stays one.  Rare, hence slow and simple.
+template <typename T, int KT>
+__device__ __noinline__ float pg_nonfinite(const PgAttend& p, const PgPiece& pc, int pos, int e) {
+    const PgSpan span = pg_span<KT>(pc.pmin, pc.pmax, p.window, p.sinks);
+    float add = 0.f;
+    for (int i = pc.i0; i < pc.i1; i++) {
+        const int key0 = pg_tile_key(span, i, KT);
+        if (!pg_partial<KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks)) continue;
+        for (int j = key0; j < key0 + KT; j++) {
+            if (!pg_sees(pos, j, p.window, p.sinks)) continue;
+            const long long row = pg_row_of(p.b, p.ge, pc.grp, pc.head, j);
+            if (row < 0) continue;
+            const float v = (float)((const T*)p.v)[(size_t)row * p.ge.D + e];
+            if (!isfinite(v)) add += v;
+        }
+    }
+    return add;
+}
+
 // ---- new rows into the pages ------------------------------------------------------------------------------------
 // cos/sin of pos * base^(-2i/d), [max_pos][d/2]: angles in double (far positions keep their fraction), stored as float32.
 static __global__ void __launch_bounds__(256) pg_rope_table_kernel(float2* __restrict__ cs, int max_pos, int half, double log2_base) {

@@ -66,27 +66,6 @@ __device__ __forceinline__ uint32_t pgm_finite(uint32_t x, bool* found) {
     *found |= lo || hi;
     return x;
 }
-// What feature e of the row at position `pos` gets from the non-finite elements of V among the keys it sees in
-// key tiles [i0, i1) that were multiplied without them (partial tiles).  A weight is positive, so an infinity
-// stays one.  Rare, hence slow and simple.
-template <int KT>
-__device__ __noinline__ float pg_nonfinite(const PgAttend& p, const PgPiece& pc, int pos, int e) {
-    const PgSpan span = pg_span<KT>(pc.pmin, pc.pmax, p.window, p.sinks);
-    float add = 0.f;
-    for (int i = pc.i0; i < pc.i1; i++) {
-        const int key0 = pg_tile_key(span, i, KT);
-        if (!pg_partial<KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks)) continue;
-        for (int j = key0; j < key0 + KT; j++) {
-            if (!pg_sees(pos, j, p.window, p.sinks)) continue;
-            const long long row = pg_row_of(p.b, p.ge, pc.grp, pc.head, j);
-            if (row < 0) continue;
-            const float v = __bfloat162float(((const __nv_bfloat16*)p.v)[(size_t)row * p.ge.D + e]);
-            if (!isfinite(v)) add += v;
-        }
-    }
-    return add;
-}
-
 // mbar_wait in few instructions: these kernels wait in many places, and their code competes for the instruction caches.
 __device__ __forceinline__ bool pg_wait(uint64_t* bar, uint32_t parity) {
 #pragma unroll 1
@@ -418,8 +397,8 @@ pg_attend_mma_kernel(const __grid_constant__ PgAttend p, const __grid_constant__
                 const int rp = p.b.row_pos[row];
                 if (rp < 0 || rp >= limit) continue;
                 if (fix) {
-                    acc.x += pg_nonfinite<PGM_KT>(p, pc, rp, e); acc.y += pg_nonfinite<PGM_KT>(p, pc, rp, e + 1);
-                    acc.z += pg_nonfinite<PGM_KT>(p, pc, rp, e + 2); acc.w += pg_nonfinite<PGM_KT>(p, pc, rp, e + 3);
+                    acc.x += pg_nonfinite<__nv_bfloat16, PGM_KT>(p, pc, rp, e); acc.y += pg_nonfinite<__nv_bfloat16, PGM_KT>(p, pc, rp, e + 1);
+                    acc.z += pg_nonfinite<__nv_bfloat16, PGM_KT>(p, pc, rp, e + 2); acc.w += pg_nonfinite<__nv_bfloat16, PGM_KT>(p, pc, rp, e + 3);
                 }
                 if (whole) {
                     const float inv = 1.0f / den;

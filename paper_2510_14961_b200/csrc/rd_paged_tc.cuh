@@ -548,7 +548,7 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                 // rare: what non-finite elements of V do to this row
 #pragma unroll 1
                 for (int e = 0; e < D; e++) {
-                    const float add = pg_nonfinite<KT>(p, pc, pos, e);
+                    const float add = pg_nonfinite<__nv_bfloat16, KT>(p, pc, pos, e);
                     if (add == 0.f) continue;
                     if (whole) {
                         const int oc = e / 8;
