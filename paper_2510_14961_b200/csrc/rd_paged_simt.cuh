@@ -249,7 +249,7 @@ __device__ __forceinline__ void pgs_split(float x, uint32_t* hi, uint32_t* lo) {
     *lo = pgs_tf32(x - __uint_as_float(*hi));
 }
 __device__ __forceinline__ void pgs_mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
@@ -336,20 +336,24 @@ __global__ void __launch_bounds__(PGS_THREADS, PgsMany<T, DP>::PER_SM) pg_attend
                         if constexpr (EXACT) ah[q] = __float_as_uint(x[q]);
                         else pgs_split(x[q], &ah[q], &al[q]);
                     }
+uint32_t h[NS][2], w[NS][2];                       // one product of every column block after the other: no MMA waits for the last
 #pragma unroll
                     for (int j = 0; j < NS; j++) {
-                        const float b0 = pg_to_f(kr[j * 8 * LD + k]), b1 = pg_to_f(kr[j * 8 * LD + k + 4]);
-                        if constexpr (EXACT) {
-                            pgs_mma(s[j], ah, __float_as_uint(b0), __float_as_uint(b1));
-                        } else {
-                            uint32_t h0, h1, l0, l1;
-                            pgs_split(b0, &h0, &l0);
-                            pgs_split(b1, &h1, &l1);
-                            pgs_mma(s[j], al, h0, h1);
-                            pgs_mma(s[j], ah, l0, l1);
-                            pgs_mma(s[j], ah, h0, h1);
+#pragma unroll
+                        for (int q = 0; q < 2; q++) {
+                            const float b = pg_to_f(kr[j * 8 * LD + k + 4 * q]);
+                            if constexpr (EXACT) h[j][q] = __float_as_uint(b);
+                            else pgs_split(b, &h[j][q], &w[j][q]);
                         }
                     }
+                    if constexpr (!EXACT) {
+#pragma unroll
+                        for (int j = 0; j < NS; j++) pgs_mma(s[j], al, h[j][0], h[j][1]);
+#pragma unroll
+                        for (int j = 0; j < NS; j++) pgs_mma(s[j], ah, w[j][0], w[j][1]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < NS; j++) pgs_mma(s[j], ah, h[j][0], h[j][1]);
                 }
             }
             __syncthreads();                                   // K(i) has been read
@@ -405,23 +409,25 @@ __global__ void __launch_bounds__(PGS_THREADS, PgsMany<T, DP>::PER_SM) pg_attend
                     pgs_split(s[j][1], &ah[2], &al[2]); pgs_split(s[j][3], &ah[3], &al[3]);
                     const T* vr = Vs + (kh * KH + j * 8 + 2 * tq) * LD + g;
 #pragma unroll
-                    for (int n = 0; n < NO; n++) {
-                        float b0 = pg_to_f(vr[n * 8]), b1 = pg_to_f(vr[LD + n * 8]);
-                        if (partial) {
-                            if (!isfinite(b0)) { b0 = 0.f; found = true; }
-                            if (!isfinite(b1)) { b1 = 0.f; found = true; }
+                    for (int n0 = 0; n0 < NO; n0 += 4) {
+                        uint32_t h[4][2], w[4][2];
+#pragma unroll
+                        for (int n = 0; n < 4; n++)
+#pragma unroll
+                            for (int q = 0; q < 2; q++) {
+                                float b = pg_to_f(vr[q * LD + (n0 + n) * 8]);
+                                if (partial && !isfinite(b)) { b = 0.f; found = true; }
+                                if constexpr (EXACT) h[n][q] = __float_as_uint(b);
+                                else pgs_split(b, &h[n][q], &w[n][q]);
+                            }
+#pragma unroll
+                        for (int n = 0; n < 4; n++) pgs_mma(o[n0 + n], al, h[n][0], h[n][1]);
+                        if constexpr (!EXACT) {
+#pragma unroll
+                            for (int n = 0; n < 4; n++) pgs_mma(o[n0 + n], ah, w[n][0], w[n][1]);
                         }
-                        if constexpr (EXACT) {
-                            pgs_mma(o[n], al, __float_as_uint(b0), __float_as_uint(b1));
-                            pgs_mma(o[n], ah, __float_as_uint(b0), __float_as_uint(b1));
-                        } else {
-                            uint32_t h0, h1, l0, l1;
-                            pgs_split(b0, &h0, &l0);
-                            pgs_split(b1, &h1, &l1);
-                            pgs_mma(o[n], al, h0, h1);
-                            pgs_mma(o[n], ah, l0, l1);
-                            pgs_mma(o[n], ah, h0, h1);
-                        }
+#pragma unroll
+                        for (int n = 0; n < 4; n++) pgs_mma(o[n0 + n], ah, h[n][0], h[n][1]);
                     }
                 }
             }
