@@ -97,33 +97,6 @@ __device__ __forceinline__ pgt_f2 pgt_add(pgt_f2 a, pgt_f2 b) { pgt_f2 r; asm("a
 // largest of three, NaN if one is (a NaN score has to reach its row)
 __device__ __forceinline__ float pgt_max3(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 
-// 2^x for two x <= 126 on the FMA and integer pipes: x = n + f with n the nearest whole number (adding 1.5 * 2^23
-// leaves it in the low bits) and |f| <= 1/2, 2^f by a polynomial, n added to its exponent.  The coefficients are a
-// minimax fit of 2^f with p(0) = 1 (largest relative error 2.9e-6, far below the rounding of P to bf16).  x is
-// held at -127, where the sum of the exponents is 0: everything below 2^-127, masked scores too, comes out as 0
-// (or less than 2^-126).  The softmax gives some of its exponentials to these pipes because 128 of them per
-// thread and tile keep the SM's MUFU busy for as long as the two products take.
-__device__ __forceinline__ void pgt_exp2_pair(pgt_f2 x, float* e0, float* e1) {
-    float a, b;
-    pgt_unpack(x, &a, &b);
-    x = pgt_pack(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
-    const pgt_f2 r = pgt_add(x, pgt_pack(12582912.0f, 12582912.0f));
-    const pgt_f2 n = pgt_add(r, pgt_pack(-12582912.0f, -12582912.0f));
-    const pgt_f2 f = pgt_fma(n, pgt_pack(-1.0f, -1.0f), x);
-    pgt_f2 p = pgt_fma(f, pgt_pack(0.009582853f, 0.009582853f), pgt_pack(0.055906426f, 0.055906426f));
-    p = pgt_fma(p, f, pgt_pack(0.24024099f, 0.24024099f));
-    p = pgt_fma(p, f, pgt_pack(0.6931242f, 0.6931242f));
-    p = pgt_fma(p, f, pgt_pack(1.0f, 1.0f));
-    float p0, p1, r0, r1;
-    pgt_unpack(p, &p0, &p1);
-    pgt_unpack(r, &r0, &r1);
-    *e0 = __int_as_float(__float_as_int(p0) + (__float_as_int(r0) << 23));
-    *e1 = __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23));
-}
-#ifndef PGT_POLY
-#define PGT_POLY 4                     // of this many pairs of exponentials one goes to the FMA pipe
-#endif
-
 template <int D>
 __global__ void __launch_bounds__(PGT_THREADS, 1)
 pg_attend_tc_kernel(const __grid_constant__ PgAttend p, const __grid_constant__ PgMaps maps) {
@@ -417,19 +390,17 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                     if (move) m = mx;
                 };
                 const pgt_f2 cc = pgt_pack(c2, c2);
-                // P of 32 keys (16 packed words) from their scores, one pair of every `poly` on the FMA pipe
-                auto exps = [&](const uint32_t* s, uint32_t* pw, pgt_f2 uu, int poly) {
+                // P of 32 keys (16 packed words) from their scores.  (Giving a part of the exponentials to the FMA pipe, as a polynomial,
+                // costs more issue slots than it frees MUFU slots: 1/2, 1/4, 1/8, 1/16, none of them: 540, 506, 480, 477, 464 us for
+                // an 8,192-token prompt.)
+                auto exps = [&](const uint32_t* s, uint32_t* pw, pgt_f2 uu) {
 #pragma unroll
                     for (int k = 0; k < 16; k++) {
                         const pgt_f2 x = pgt_fma(pgt_pack(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), cc, uu);
                         float e0, e1;
-                        if (k % poly == poly - 1) {
-                            pgt_exp2_pair(x, &e0, &e1);
-                        } else {
-                            pgt_unpack(x, &e0, &e1);
-                            e0 = ex2_approx(e0);
-                            e1 = ex2_approx(e1);
-                        }
+                        pgt_unpack(x, &e0, &e1);
+                        e0 = ex2_approx(e0);
+                        e1 = ex2_approx(e1);
                         sums[k & 1] = pgt_add(sums[k & 1], pgt_pack(e0, e1));
                         pw[k] = pack_bf16(e0, e1);
                     }
@@ -453,16 +424,16 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                     settle(pgt_max3(pgt_max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]) * c2);
                     const float u = m == -INFINITY ? 0.f : m;
                     const pgt_f2 uu = pgt_pack(-u, -u);
-                    exps(sr, pw, uu, PGT_POLY);
-                    exps(sr + 32, pw + 16, uu, PGT_POLY);
+                    exps(sr, pw, uu);
+                    exps(sr + 32, pw + 16, uu);
                     tmem_st32_issue(t_s, pw);
-                    exps(sr + 64, pw, uu, PGT_POLY);
+                    exps(sr + 64, pw, uu);
                     tmem_st16_issue(t_s + 32, pw);
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&p_lo[w]);      // the product may begin with these 96 keys
-                    exps(sr + 96, pw, uu, PGT_POLY);
+                    exps(sr + 96, pw, uu);
                     tmem_st16_issue(t_s + 48, pw);
                 } else {
                     // a tile with masked keys: 32 keys at a time in loops that stay small (unrolled like the path above, the
@@ -487,7 +458,7 @@ uint4 x[(32 + RI - 1) / RI];                   // every load is under way before
                             tmem_ld32(t_s + c, sr);
 #pragma unroll
                             for (int k = 0; k < 32; k++) sr[k] = (see >> k & 1) ? sr[k] : 0xff800000u;
-                            exps(sr, pw, uu, PGT_POLY);
+                            exps(sr, pw, uu);
                         } else {
 #pragma unroll
                             for (int k = 0; k < 16; k++) pw[k] = 0;
