@@ -297,7 +297,7 @@ static int attend_part(rd_paged* c, PgAttend a, bool many, int m, cudaStream_t s
     }
     a.min_share = 1;
     a.item_cost = 2;
-    a.whole_units = 4;
+    a.whole_units = 2;
     return c->cfg.dtype == RD_BF16 ? attend_simt_d<bf16>(c, a, many, st, chained, launches) : attend_simt_d<float>(c, a, many, st, chained, launches);
 }
 

@@ -1,22 +1,18 @@
-// Attention over a paged cache in float32, and in bf16 with head sizes the kernels on tcgen05 and bf16 mma.sync do not
-// take.  Any even head_dim up to DP = 32, 64, 96 or 128 (shared-memory rows are padded with zeros).  Arguments, row tiles
-// and the division of the work: rd_paged.cuh.
+// Attention over a paged cache on the CUDA cores: float32 (whose products the tensor cores would round), and
+// bf16 with head sizes the tensor-core kernels do not take.  Any even head_dim up to DP = 32, 64, 96 or 128
+// (shared-memory rows are padded with zeros).  Arguments, row tiles and the division of the work: rd_paged.cuh.
 //
-// pg_attend_few_kernel (row tiles of 16): CUDA cores, bound by the K/V stream.  A 64-key tile is eight runs of 8 keys, one
+// pg_attend_few_kernel (row tiles of 16): bound by the K/V stream.  A 64-key tile is eight runs of 8 keys, one
 //   per warp; a warp brings its run in by itself (16-byte cp.async, three stages of its own) and keeps its own
 //   maximum, sum and output, so no warp waits for another before the end of an item.  Four lanes share a key's
 //   dot product, a lane owns DP / 32 output features.
-// pg_attend_many_kernel (row tiles of 64): mma.sync m16n8k8 in tf32 with every float32 operand as a sum of two tf32
-//   numbers (x = hi + lo up to 2^-22 |x|): hi hi + hi lo + lo hi, accumulated in float32, errs by about 2^-21 of a
-//   product, next to the 2^-24 of an FMA chain's every step; bf16 operands are tf32 numbers already.  (The same tile on FMAs
-//   took 7 us: 1,024 FMAs and 160 shared-memory reads per warp for the scores alone.)  Four blocks of 16 rows x two halves of
-//   a 64-key tile; the halves keep (m, l, O) of their own and meet at the end of a piece.  P goes from the
-//   accumulators of S into the A operand of P V as it lies: an 8-key step of that product takes the keys in the
-//   order 0 2 4 6 1 3 5 7, for P and V alike.  K(t + 1) is requested behind Q K^T of tile t and V(t + 1) behind P V, so
-//   one buffer each suffices.
+// pg_attend_many_kernel (row tiles of 64): bound by the FMA rate.  Eight warps own 8 rows each; a lane takes
+//   keys `lane` and `lane + 32` of the tile for 8 rows (16 FMAs per two K and eight Q reads of 4 floats, the Q
+//   reads being broadcasts), then DP / 32 output features for 8 rows.  K(t + 1) is requested behind Q K^T of
+//   tile t and V(t + 1) behind P V, so one buffer each suffices.
 //
-// Keys that some row of a tile does not see: the first kernel never multiplies by them; the second takes non-finite
-// elements of V out of such tiles and gives them to the rows that see them at the end (pg_nonfinite).
+// A key no row of the tile sees is never multiplied: masked probabilities skip the V row, so what lies in
+// unwritten places of a page does not matter.
 #pragma once
 #include "rd_paged.cuh"
 
@@ -238,41 +234,27 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_few_kernel(const __g
 template <typename T, int DP> struct PgsMany {
     static constexpr int LD = DP + 16 / (int)sizeof(T);
     static constexpr int TILE = PGS_KT * LD * (int)sizeof(T);
-    static constexpr int QLD = DP + 4;
-    static constexpr int SMEM = 2 * TILE + 2 * PGS_MANY * QLD * 4 + PGS_MANY * 8;      // K, V, Q, the second halves' O and (m, l)
+    static constexpr int QLD = DP + 4, PLD = PGS_KT + 4;
+    static constexpr int SMEM = 2 * TILE + PGS_MANY * QLD * 4 + PGS_MANY * PLD * 4;
     static constexpr int PER_SM = DP <= 64 ? 2 : 1;
 };
-
-__device__ __forceinline__ uint32_t pgs_tf32(float x) { uint32_t r; asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x)); return r; }
-__device__ __forceinline__ void pgs_split(float x, uint32_t* hi, uint32_t* lo) {
-    *hi = pgs_tf32(x);
-    *lo = pgs_tf32(x - __uint_as_float(*hi));
-}
-__device__ __forceinline__ void pgs_mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 
 // Two blocks share an SM where their tiles fit (head_dim up to 64): one block's barriers hide behind the other's work.
 template <typename T, int DP>
 __global__ void __launch_bounds__(PGS_THREADS, PgsMany<T, DP>::PER_SM) pg_attend_many_kernel(const __grid_constant__ PgAttend p) {
     using C = PgsMany<T, DP>;
-    constexpr int M = PGS_MANY, LD = C::LD, QLD = C::QLD, NO = DP / 8, KH = PGS_KT / 2, NS = KH / 8;
-    constexpr bool EXACT = sizeof(T) == 2;                     // bf16 operands need no second part
+    constexpr int M = PGS_MANY, LD = C::LD, QLD = C::QLD, PLD = C::PLD, E = DP / 32, RW = 8;
     extern __shared__ __align__(16) uint8_t pgs_raw[];
     T* Ks = reinterpret_cast<T*>(pgs_raw);
     T* Vs = reinterpret_cast<T*>(pgs_raw + C::TILE);
     float* Qs = reinterpret_cast<float*>(pgs_raw + 2 * C::TILE);
-    float* Os = Qs + M * QLD;
-    float* MLs = Os + M * QLD;
+    float* Ps = Qs + M * QLD;
     __shared__ PgPlanSmem<PG_INLINE_REC> plan;
-    __shared__ int flag, found_s;
+    __shared__ int flag;
     pdl_enter();
-    if (threadIdx.x == 0) found_s = 0;
     pg_plan_share<PGS_THREADS, PGS_KT>(p, M, plan);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, D = p.ge.D, g = lane >> 2, tq = lane & 3;
-    const int limit = pg_pos_limit(p.b, p.ge), qb = warp & 3, kh = warp >> 2, kl = tid >> 2;
-    const float c2 = p.scale_log2;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, D = p.ge.D;
+    const int limit = pg_pos_limit(p.b, p.ge), r_w = warp * RW, kl = tid >> 2;
     PgsKey key;
     key.bad = false;
     auto sync = [] { __syncthreads(); };
@@ -285,7 +267,7 @@ __global__ void __launch_bounds__(PGS_THREADS, PgsMany<T, DP>::PER_SM) pg_attend
         const PgSpan span = pg_span<PGS_KT>(pc.pmin, pc.pmax, p.window, p.sinks);
         const int rows = (int)min((long long)M, (long long)pc.n * p.ge.g - (long long)pc.rt * M);
         const int lo_key = p.window > 0 ? max(0, pc.pmin - p.window + 1) : 0;
-        // four threads bring one key's row in; `row_k` is where the tile whose K was asked for last lies
+        // four threads bring one key's row in; `row` is where the tile whose K was asked for last lies
         key.ask(p, pc, span, lo_key, pc.i0, kl);
         long long row_k = -1;
         auto load_k = [&](int i) {
@@ -304,188 +286,142 @@ __global__ void __launch_bounds__(PGS_THREADS, PgsMany<T, DP>::PER_SM) pg_attend
             const int r = i / DP, e = i % DP;
             float x = 0.f;
             if (r < rows && e < D) {
-                const unsigned pk = (unsigned)pc.rt * M + r, of = pk / (unsigned)p.ge.g;
-                x = pg_to_f(((const T*)p.q)[(size_t)(pc.a + (int)of) * p.ldq + (size_t)(pc.head * p.ge.g + (int)(pk - of * p.ge.g)) * D + e]);
+                const long long pk = (long long)pc.rt * M + r;
+                x = pg_to_f(((const T*)p.q)[(size_t)(pc.a + pk / p.ge.g) * p.ldq + (size_t)(pc.head * p.ge.g + pk % p.ge.g) * D + e]) * p.scale_log2;
             }
             Qs[r * QLD + e] = x;
         }
-        // this thread's rows: qb * 16 + g and 8 further on
-        const int pos_a = pgs_row_position(p, pc, M, qb * 16 + g, limit), pos_b = pgs_row_position(p, pc, M, qb * 16 + g + 8, limit);
-        const int low_a = pg_window_lo(pos_a, p.window), low_b = pg_window_lo(pos_b, p.window);
-        float m_a = -INFINITY, m_b = -INFINITY, l_a = 0.f, l_b = 0.f, o[NO][4];
+        int pos[RW];
+        float m[RW], l[RW], o[RW][E];
 #pragma unroll
-        for (int j = 0; j < NO; j++) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-        bool found = false;
-        const bool work = qb * 16 < rows;                      // warps whose rows are all padding only help loading
+        for (int r = 0; r < RW; r++) {
+            pos[r] = pgs_row_position(p, pc, M, r_w + r, limit);
+            m[r] = -INFINITY; l[r] = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; e++) o[r][e] = 0.f;
+        }
+        const bool work = r_w < rows;                              // warps whose rows are all padding only help loading
         for (int i = pc.i0; i < pc.i1; i++) {
-            const int key0 = pg_tile_key(span, i, PGS_KT) + kh * KH;
+            const int key0 = pg_tile_key(span, i, PGS_KT);
             pgs_wait<1>();
-            __syncthreads();                                   // K(i) and Q are there
-            float s[NS][4];
+            __syncthreads();                                       // K(i) and Q are there
+            float s[RW][2];
             if (work) {
 #pragma unroll
-                for (int j = 0; j < NS; j++) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-                const float* qr = Qs + (qb * 16 + g) * QLD + tq;
-                const T* kr = Ks + (kh * KH + g) * LD + tq;
+                for (int r = 0; r < RW; r++) s[r][0] = s[r][1] = 0.f;
 #pragma unroll 4
-                for (int k = 0; k < DP; k += 8) {
-                    uint32_t ah[4], al[4];
-                    const float x[4] = {qr[k], qr[8 * QLD + k], qr[k + 4], qr[8 * QLD + k + 4]};
+                for (int c = 0; c < DP / 4; c++) {
+                    float k0[4], k1[4];
+                    pgs_f4(Ks + lane * LD + c * 4, k0);
+                    pgs_f4(Ks + (lane + 32) * LD + c * 4, k1);
 #pragma unroll
-                    for (int q = 0; q < 4; q++) {
-                        if constexpr (EXACT) ah[q] = __float_as_uint(x[q]);
-                        else pgs_split(x[q], &ah[q], &al[q]);
+                    for (int r = 0; r < RW; r++) {
+                        const float4 q = *reinterpret_cast<const float4*>(Qs + (r_w + r) * QLD + c * 4);
+                        s[r][0] = fmaf(q.x, k0[0], s[r][0]); s[r][0] = fmaf(q.y, k0[1], s[r][0]);
+                        s[r][0] = fmaf(q.z, k0[2], s[r][0]); s[r][0] = fmaf(q.w, k0[3], s[r][0]);
+                        s[r][1] = fmaf(q.x, k1[0], s[r][1]); s[r][1] = fmaf(q.y, k1[1], s[r][1]);
+                        s[r][1] = fmaf(q.z, k1[2], s[r][1]); s[r][1] = fmaf(q.w, k1[3], s[r][1]);
                     }
-uint32_t h[NS][2], w[NS][2];                       // one product of every column block after the other: no MMA waits for the last
-#pragma unroll
-                    for (int j = 0; j < NS; j++) {
-#pragma unroll
-                        for (int q = 0; q < 2; q++) {
-                            const float b = pg_to_f(kr[j * 8 * LD + k + 4 * q]);
-                            if constexpr (EXACT) h[j][q] = __float_as_uint(b);
-                            else pgs_split(b, &h[j][q], &w[j][q]);
-                        }
-                    }
-                    if constexpr (!EXACT) {
-#pragma unroll
-                        for (int j = 0; j < NS; j++) pgs_mma(s[j], al, h[j][0], h[j][1]);
-#pragma unroll
-                        for (int j = 0; j < NS; j++) pgs_mma(s[j], ah, w[j][0], w[j][1]);
-                    }
-#pragma unroll
-                    for (int j = 0; j < NS; j++) pgs_mma(s[j], ah, h[j][0], h[j][1]);
                 }
             }
-            __syncthreads();                                   // K(i) has been read
+            __syncthreads();                                       // K(i) has been read
             load_k(i + 1);
-            const bool partial = pg_partial<PGS_KT>(key0 - kh * KH, pc.pmin, pc.pmax, p.window, p.sinks);
             if (work) {
-                if (partial) {
-                    const uint32_t see_a = pg_see_bits(key0, pos_a, low_a, p.sinks), see_b = pg_see_bits(key0, pos_b, low_b, p.sinks);
 #pragma unroll
-                    for (int j = 0; j < NS; j++) {
-                        const int k0 = j * 8 + 2 * tq;
-                        s[j][0] = (see_a >> k0 & 1) ? s[j][0] : -INFINITY;
-                        s[j][1] = (see_a >> k0 & 2) ? s[j][1] : -INFINITY;
-                        s[j][2] = (see_b >> k0 & 1) ? s[j][2] : -INFINITY;
-                        s[j][3] = (see_b >> k0 & 2) ? s[j][3] : -INFINITY;
+                for (int r = 0; r < RW; r++) {
+                    const bool v0 = pos[r] >= 0 && pg_sees(pos[r], key0 + lane, p.window, p.sinks);
+                    const bool v1 = pos[r] >= 0 && pg_sees(pos[r], key0 + lane + 32, p.window, p.sinks);
+                    float mx = fmaxf(v0 ? s[r][0] : -INFINITY, v1 ? s[r][1] : -INFINITY);
+#pragma unroll
+                    for (int w = 1; w < 32; w *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                    if (mx > m[r]) {
+                        const float f = exp2f(m[r] - mx);
+                        l[r] *= f;
+#pragma unroll
+                        for (int e = 0; e < E; e++) o[r][e] *= f;
+                        m[r] = mx;
                     }
+                    const float p0 = v0 ? exp2f(s[r][0] - m[r]) : 0.f, p1 = v1 ? exp2f(s[r][1] - m[r]) : 0.f;
+                    l[r] += p0 + p1;
+                    Ps[(r_w + r) * PLD + lane] = p0;
+                    Ps[(r_w + r) * PLD + lane + 32] = p1;
                 }
-                float mx_a = -INFINITY, mx_b = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < NS; j++) {
-                    mx_a = fmaxf(mx_a, fmaxf(s[j][0], s[j][1]));
-                    mx_b = fmaxf(mx_b, fmaxf(s[j][2], s[j][3]));
-                }
-#pragma unroll
-                for (int w = 1; w < 4; w *= 2) {
-                    mx_a = fmaxf(mx_a, __shfl_xor_sync(0xffffffffu, mx_a, w));
-                    mx_b = fmaxf(mx_b, __shfl_xor_sync(0xffffffffu, mx_b, w));
-                }
-                const float mn_a = fmaxf(m_a, mx_a * c2), mn_b = fmaxf(m_b, mx_b * c2);
-                const float ua = mn_a == -INFINITY ? 0.f : mn_a, ub = mn_b == -INFINITY ? 0.f : mn_b;
-                const float ca = exp2f(m_a - ua), cb = exp2f(m_b - ub);
-                m_a = mn_a; m_b = mn_b;
-                float sa = 0.f, sb = 0.f;
-#pragma unroll
-                for (int j = 0; j < NS; j++) {
-                    s[j][0] = exp2f(fmaf(s[j][0], c2, -ua)); s[j][1] = exp2f(fmaf(s[j][1], c2, -ua));
-                    s[j][2] = exp2f(fmaf(s[j][2], c2, -ub)); s[j][3] = exp2f(fmaf(s[j][3], c2, -ub));
-                    sa += s[j][0] + s[j][1];
-                    sb += s[j][2] + s[j][3];
-                }
-                l_a = l_a * ca + sa;
-                l_b = l_b * cb + sb;
-#pragma unroll
-                for (int j = 0; j < NO; j++) { o[j][0] *= ca; o[j][1] *= ca; o[j][2] *= cb; o[j][3] *= cb; }
             }
             pgs_wait<1>();
-            __syncthreads();                                   // V(i) is there
+            __syncthreads();                                       // V(i) is there (and the warp's own P)
             if (work) {
+                // four keys at a time; a tile with a key that some row does not see goes key by key when V is not finite all
+                // over it (0 times an infinity would be a NaN)
+                bool fast = true;
+                if (pg_partial<PGS_KT>(key0, pc.pmin, pc.pmax, p.window, p.sinks)) {
+                    float probe = 0.f;
+#pragma unroll 4
+                    for (int j = 0; j < PGS_KT; j++)
 #pragma unroll
-                for (int j = 0; j < NS; j++) {
-                    uint32_t ah[4], al[4];
-                    pgs_split(s[j][0], &ah[0], &al[0]); pgs_split(s[j][2], &ah[1], &al[1]);
-                    pgs_split(s[j][1], &ah[2], &al[2]); pgs_split(s[j][3], &ah[3], &al[3]);
-                    const T* vr = Vs + (kh * KH + j * 8 + 2 * tq) * LD + g;
+                        for (int e = 0; e < E; e++) probe = fmaf(pg_to_f(Vs[j * LD + lane + 32 * e]), 0.f, probe);
+                    fast = __all_sync(0xffffffffu, probe == 0.f);
+                }
+                if (fast) {
+#pragma unroll 2
+                    for (int j = 0; j < PGS_KT; j += 4) {
+                        float v[4][E];
 #pragma unroll
-                    for (int n0 = 0; n0 < NO; n0 += 4) {
-                        uint32_t h[4][2], w[4][2];
+                        for (int t = 0; t < 4; t++)
 #pragma unroll
-                        for (int n = 0; n < 4; n++)
+                            for (int e = 0; e < E; e++) v[t][e] = pg_to_f(Vs[(j + t) * LD + lane + 32 * e]);
 #pragma unroll
-                            for (int q = 0; q < 2; q++) {
-                                float b = pg_to_f(vr[q * LD + (n0 + n) * 8]);
-                                if (partial && !isfinite(b)) { b = 0.f; found = true; }
-                                if constexpr (EXACT) h[n][q] = __float_as_uint(b);
-                                else pgs_split(b, &h[n][q], &w[n][q]);
+                        for (int r = 0; r < RW; r++) {
+                            const float4 w = *reinterpret_cast<const float4*>(Ps + (r_w + r) * PLD + j);
+#pragma unroll
+                            for (int e = 0; e < E; e++) {
+                                o[r][e] = fmaf(w.x, v[0][e], o[r][e]); o[r][e] = fmaf(w.y, v[1][e], o[r][e]);
+                                o[r][e] = fmaf(w.z, v[2][e], o[r][e]); o[r][e] = fmaf(w.w, v[3][e], o[r][e]);
                             }
-#pragma unroll
-                        for (int n = 0; n < 4; n++) pgs_mma(o[n0 + n], al, h[n][0], h[n][1]);
-                        if constexpr (!EXACT) {
-#pragma unroll
-                            for (int n = 0; n < 4; n++) pgs_mma(o[n0 + n], ah, w[n][0], w[n][1]);
                         }
+                    }
+                } else {
+                    for (int j = 0; j < PGS_KT; j++) {
+                        const int key = key0 + j;
 #pragma unroll
-                        for (int n = 0; n < 4; n++) pgs_mma(o[n0 + n], ah, h[n][0], h[n][1]);
+                        for (int r = 0; r < RW; r++) {
+                            if (pos[r] < 0 || !pg_sees(pos[r], key, p.window, p.sinks)) continue;
+                            const float w = Ps[(r_w + r) * PLD + j];
+#pragma unroll
+                            for (int e = 0; e < E; e++) o[r][e] = fmaf(w, pg_to_f(Vs[j * LD + lane + 32 * e]), o[r][e]);
+                        }
                     }
                 }
             }
-            __syncthreads();                                   // V(i) has been read
+            __syncthreads();                                       // V(i) has been read
             load_v();
         }
         pgs_wait<0>();
-        if (found) found_s = 1;
-        // the two halves of the keys meet: the second's results through shared memory
-#pragma unroll
-        for (int w = 1; w < 4; w *= 2) {
-            l_a += __shfl_xor_sync(0xffffffffu, l_a, w);
-            l_b += __shfl_xor_sync(0xffffffffu, l_b, w);
-        }
-        const int ra = qb * 16 + g;
-        if (kh == 1 && work) {
-#pragma unroll
-            for (int n = 0; n < NO; n++) {
-                *reinterpret_cast<float2*>(Os + ra * QLD + n * 8 + 2 * tq) = make_float2(o[n][0], o[n][1]);
-                *reinterpret_cast<float2*>(Os + (ra + 8) * QLD + n * 8 + 2 * tq) = make_float2(o[n][2], o[n][3]);
-            }
-            if (tq == 0) {
-                *reinterpret_cast<float2*>(MLs + 2 * ra) = make_float2(m_a, l_a);
-                *reinterpret_cast<float2*>(MLs + 2 * (ra + 8)) = make_float2(m_b, l_b);
-            }
-        }
-        __syncthreads();
-        const bool whole = pc.c_first == pc.c_last, fix = found_s != 0;
+        const bool whole = pc.c_first == pc.c_last;
         float* slot = whole ? nullptr : pg_slot(p.w, blockIdx.x, pc.c_first, M, D);
-        if (kh == 0 && work) {
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const int r = ra + 8 * h, pos = h ? pos_b : pos_a;
-                if (pos < 0) continue;
-                const unsigned pk = (unsigned)pc.rt * M + r, of = pk / (unsigned)p.ge.g;
-                const int row = pc.a + (int)of, hd = pc.head * p.ge.g + (int)(pk - of * p.ge.g);
-                const float2 ml = *reinterpret_cast<const float2*>(MLs + 2 * r);
-                const float m = h ? m_b : m_a, mx = fmaxf(m, ml.x), u = mx == -INFINITY ? 0.f : mx;
-                const float f0 = exp2f(m - u), f1 = exp2f(ml.x - u), den = (h ? l_b : l_a) * f0 + ml.y * f1, inv = whole ? 1.0f / den : 1.0f;
+        for (int r = 0; r < RW; r++) {
+            float ls = l[r];
 #pragma unroll
-                for (int n = 0; n < NO; n++) {
-                    const int e = n * 8 + 2 * tq;
-                    if (e >= D) continue;                       // (D is even)
-                    const float2 x = *reinterpret_cast<const float2*>(Os + r * QLD + e);
-                    float y0 = o[n][2 * h] * f0 + x.x * f1, y1 = o[n][2 * h + 1] * f0 + x.y * f1;
-                    if (fix) { y0 += pg_nonfinite<T, PGS_KT>(p, pc, pos, e); y1 += pg_nonfinite<T, PGS_KT>(p, pc, pos, e + 1); }
-                    if (whole) pg_set_pair((T*)p.out + (size_t)row * p.ldo + (size_t)hd * D + e, y0 * inv, y1 * inv);
-                    else *reinterpret_cast<float2*>(slot + (size_t)r * D + e) = make_float2(y0, y1);
-                }
-                if (tq == 0) {
-                    if (!whole) *reinterpret_cast<float2*>(slot + (size_t)M * D + 2 * r) = make_float2(mx, den);
-                    else if (p.lse) p.lse[(size_t)row * p.ge.n_heads + hd] = (mx + log2f(den)) * 0.6931471805599453f;
-                }
+            for (int w = 1; w < 32; w *= 2) ls += __shfl_xor_sync(0xffffffffu, ls, w);
+            const int rr = r_w + r;
+            if (rr >= rows) continue;
+            const long long pk = (long long)pc.rt * M + rr;
+            const int row = pc.a + (int)(pk / p.ge.g), hd = pc.head * p.ge.g + (int)(pk % p.ge.g);
+            if (whole) {
+                if (pos[r] < 0) continue;
+#pragma unroll
+                for (int e = 0; e < E; e++)
+                    if (lane + 32 * e < D) ((T*)p.out)[(size_t)row * p.ldo + (size_t)hd * D + lane + 32 * e] = pg_from_f<T>(o[r][e] / ls);
+                if (p.lse && lane == 0) p.lse[(size_t)row * p.ge.n_heads + hd] = (m[r] + log2f(ls)) * 0.6931471805599453f;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; e++)
+                    if (lane + 32 * e < D) slot[(size_t)rr * D + lane + 32 * e] = o[r][e];
+                if (lane == 0) { slot[(size_t)M * D + 2 * rr] = m[r]; slot[(size_t)M * D + 2 * rr + 1] = ls; }
             }
         }
         if (!whole && pg_arrive_last(p.w, pc, tid == 0, &flag, sync)) pg_join_any<T>(p, pc, M, D, tid, PGS_THREADS);
         __syncthreads();
-        if (tid == 0) found_s = 0;
     }
     if (key.bad) atomicOr(p.w.status, PG_ST_BAD_PAGE);
 }
