@@ -370,13 +370,15 @@ typedef struct {
 
 /* rd_paged_create -- a cache on the current device.
  *   k_pages, v_pages  device memory [n_layers][n_pages][n_kv_heads][page_size][head_dim] each, 16-byte
- *                 aligned, that the caller keeps alive as long as the cache (several caches may share it);
+ *                 aligned and apart, that the caller keeps alive as long as the cache (several caches may share it);
  *                 both NULL: the library allocates it, zero-filled (rd_paged_pages tells where).
  * One workspace belongs to the cache: its calls must run one after another (one stream, or streams that the
  * caller orders; likewise replays of CUDA graphs that captured them).  Work that is to overlap takes a
- * cache of its own over the same pages.  Calls allocate nothing, synchronise nothing and may be captured.
+ * cache of its own over the same pages.  rd_paged_append and rd_paged_attend allocate nothing, synchronise
+ * nothing and may be captured into a graph.
  * Errors: INVALID_ARG, OOM, CUDA, CAPACITY (more than 2^31 - 512 pool rows
- * n_layers * n_pages * n_kv_heads * page_size). */
+ * n_layers * n_pages * n_kv_heads * page_size, max_context above 2^30, max_rows above 2^24 or
+ * max_rows * n_heads / n_kv_heads above 10^9). */
 int rd_paged_create(const rd_paged_config* cfg, void* k_pages, void* v_pages, rd_paged** out);
 /* Waits for the device, then frees what the library allocated. */
 void rd_paged_destroy(rd_paged* c);

@@ -154,9 +154,12 @@ extern "C" int rd_paged_create(const rd_paged_config* cfg, void* k_pages, void* 
     if (g.page_size < 16 || g.page_size > 256 || (g.page_size & (g.page_size - 1))) return RD_E_INVALID_ARG;
     if (g.n_pages < 1 || g.n_layers < 1 || g.max_context < 1 || g.max_rows < 0 || !(g.rope_base >= 0.f) || !isfinite(g.rope_base)) return RD_E_INVALID_ARG;
     if (g.n_heads > 65536 || g.n_kv_heads > 65536 || ((uintptr_t)k_pages & 15) || ((uintptr_t)v_pages & 15)) return RD_E_INVALID_ARG;
+    if (g.max_context > (1 << 30)) return RD_E_CAPACITY;
     // TMA names pool rows by 32-bit coordinates
     const double rows = (double)g.n_layers * g.n_pages * g.n_kv_heads * g.page_size;
     if (rows > 2147483647.0 - 512.0) return RD_E_CAPACITY;
+    const size_t pool = (size_t)rows * g.head_dim * (g.dtype == RD_BF16 ? 2 : 4);
+    if (k_pages && (uintptr_t)k_pages < (uintptr_t)v_pages + pool && (uintptr_t)v_pages < (uintptr_t)k_pages + pool) return RD_E_INVALID_ARG;
     if (g.max_rows == 0) g.max_rows = 65536;
     // packed rows (rows x query heads per K/V head) are counted in 31 bits
     if (g.max_rows > (1 << 24) || (double)g.max_rows * (g.n_heads / g.n_kv_heads) > 1e9) return RD_E_CAPACITY;
@@ -286,6 +289,12 @@ template <typename T> static int attend_simt_d(rd_paged* c, const PgAttend& a, b
     return attend_simt<T, 128>(c, a, many, st, chained, launches);
 }
 static int attend_part(rd_paged* c, PgAttend a, bool many, int m, cudaStream_t st, bool chained, int* launches) {
+    // The division's three numbers (rd_paged.cuh), in key tiles of the kernel, as measured:
+    // few rows, tiles of 32 keys: an item's query, output and pipeline refill cost as much as 12 tiles (64 ragged tokens: 171 us
+    // counted as 2, 130 as 6, 118 as 12); up to 40 tiles an item is faster alone than cut and joined (one token behind 543
+    // positions, 55 heads: 17.5 us cut, 12.4 whole; one behind 1,000 on 8 heads: 13.3 cut, 17.1 whole).
+    // many rows, tiles of 128 keys: 4 tiles (8,192-token prompt: 606 us counted as 2, 491 as 4 or 6), whole up to 8 (128 rows
+    // behind 300 positions x 8: 35.6 cut, 25.7 whole).
     if (c->tensor) {
         a.min_share = many ? 1 : 8;
         a.item_cost = many ? 4 : 12;
@@ -295,6 +304,8 @@ static int attend_part(rd_paged* c, PgAttend a, bool many, int m, cudaStream_t s
         return a.ge.D == 64 ? attend_few_tensor<64>(c, a, m, st, chained, launches) : a.ge.D == 96 ? attend_few_tensor<96>(c, a, m, st, chained, launches)
                                                                                        : attend_few_tensor<128>(c, a, m, st, chained, launches);
     }
+    // CUDA cores, tiles of 64 keys: a tile takes longer than joining, so items are cut down to single tiles (24 rows behind 1,000
+    // positions x 4: 50 us; with at least 4 tiles a share 68, whole up to 20 tiles 154)
     a.min_share = 1;
     a.item_cost = 2;
     a.whole_units = 2;

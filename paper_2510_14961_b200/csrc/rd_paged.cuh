@@ -189,21 +189,21 @@ template <int NT, typename V> __device__ __forceinline__ V pg_block_scan(V v, V*
 // Row tiles of all groups: `first` (shared memory, n_groups entries) receives the number of the first
 // row tile of every group; returns how many there are.
 template <int NT>
-__device__ int pg_count_tiles(const PgAttend& p, int M, int* first, int* warp_sums) {
+__device__ int pg_count_tiles(const PgAttend& p, int M, int* first, long long* warp_sums) {
     const int ng = p.b.n_groups;
-    int base = 0;
+    long long base = 0;                                    // (borders that do not ascend can name rows many times over)
     for (int c0 = 0; c0 < ng; c0 += NT) {
         const int i = c0 + (int)threadIdx.x;
-        int t = 0;
+        long long t = 0;
         if (i < ng) {
             int a, n;
             pg_group_rows(p.b, i, &a, &n);
             const long long packed = (long long)n * p.ge.g;
-            if (packed > p.packed_lo && packed <= p.packed_hi) t = (int)((packed + M - 1) / M);
+            if (packed > p.packed_lo && packed <= p.packed_hi) t = (packed + M - 1) / M;
         }
-        int tot;
-        const int at = pg_block_scan<NT, int>(t, warp_sums, &tot);
-        if (i < ng) first[i] = base + at;
+        long long tot;
+        const long long at = base + pg_block_scan<NT, long long>(t, warp_sums, &tot);
+        if (i < ng) first[i] = (int)min(at, 0x7fffffffll);
         base += tot;
     }
     if (base > p.rec_cap) {
@@ -211,7 +211,7 @@ __device__ int pg_count_tiles(const PgAttend& p, int M, int* first, int* warp_su
         base = p.rec_cap;
     }
     __syncthreads();
-    return base;
+    return (int)base;
 }
 // Records r0, r0 + step, ... of the n_rec row tiles (each by `lanes` lanes) into dst.
 template <int NT, int KT>
@@ -246,7 +246,7 @@ constexpr int PG_PLAN_THREADS = 256;
 template <int KT>
 __global__ void __launch_bounds__(PG_PLAN_THREADS) pg_plan_kernel(const __grid_constant__ PgAttend p, int M) {
     extern __shared__ int first[];
-    __shared__ int warp_sums[PG_PLAN_THREADS / 32];
+    __shared__ long long warp_sums[PG_PLAN_THREADS / 32];
     pdl_enter();
     const int n_rec = pg_count_tiles<PG_PLAN_THREADS>(p, M, first, warp_sums);
     pg_make_records<PG_PLAN_THREADS, KT>(p, M, first, n_rec, p.w.rec, blockIdx.x, gridDim.x);
@@ -263,7 +263,6 @@ template <int CAP> struct PgPlanSmem {
     PgRecord rec[CAP];           // CAP = PG_INLINE_REC, or 1 for a kernel whose plan is always made before it
     int first[CAP];
     long long warp_sums[32];
-    int warp_sums_i[32];
     PgShare share;
 };
 // All NT threads call this; the plan ends in sm.share, records in sm.rec (inline) or p.w.rec.
@@ -272,7 +271,7 @@ __device__ void pg_plan_share(const PgAttend& p, int M, PgPlanSmem<CAP>& sm) {
     int n_rec;
     const PgRecord* rec = p.w.rec;
     if (CAP > 1 && p.inline_plan) {
-        n_rec = pg_count_tiles<NT>(p, M, sm.first, sm.warp_sums_i);
+        n_rec = pg_count_tiles<NT>(p, M, sm.first, sm.warp_sums);
         pg_make_records<NT, KT>(p, M, sm.first, n_rec, sm.rec, 0, 1);
         rec = sm.rec;
         __syncthreads();

@@ -463,3 +463,39 @@ def test_blocks_that_walk_over_many_items(H, G, D, page, window, sinks):
     for _ in range(20):
         c.attend(window, sinks)
         assert torch.equal(first, c.out)
+
+
+@pytest.mark.parametrize("dtype,D,n", [(F4, 64, 40), (BF, 128, 1), (BF, 128, 100)])
+def test_group_borders_that_do_not_ascend_are_survived(dtype, D, n):
+    # overlapping and reversed groups: results are undefined, every access stays inside, the call after it is right
+    c = Case(dtype, 4, 2, D, 16, [(n, 40)] * 6, seed=23)
+    good = c.start.clone()
+    for border in ([0, 6 * n, 0, 6 * n, 0, 6 * n, 0], [6 * n, 5 * n, 4 * n, 3 * n, 2 * n, n, 0], [-5, 10 ** 9, -7, 3, 2 ** 31 - 1, -2 ** 31, 6 * n]):
+        c.start.copy_(torch.tensor(border, dtype=torch.int32))
+        for call in (lambda: c.cache.attend(c.rows, c.q, c.out, c.lse), lambda: c.cache.append(c.rows, c.q, c.k, c.v, c.q_out)):
+            call()
+            try:
+                c.cache.sync()
+            except rd.RdError as err:
+                assert err.code == rd.RD_E_INVALID_ARG
+    c.start.copy_(good)
+    c.out.fill_(FILL)
+    c.attend()
+    c.check_attend()
+
+
+def test_rows_of_a_fused_projection():
+    # q, k and v as column ranges of one array, q turned in place
+    H, G, D, n = 4, 2, 64, 70
+    c = Case(BF, H, G, D, 16, [(n, 33)], seed=24)
+    buf = torch.cat([c.q, c.k, c.v], dim=1).contiguous()
+    q, k, v = buf[:, :H * D], buf[:, H * D:(H + G) * D], buf[:, (H + G) * D:]
+    c.append()
+    kp = c.kp.clone()
+    c.kp.normal_()
+    c.cache.append(c.rows, q, k, v, q)
+    c.cache.sync()
+    used = [int(x) for x in c.table_np[0]]
+    assert torch.equal(q, c.q_out)
+    for p in range(33, 33 + n):
+        assert torch.equal(c.kp[0, used[p // 16], :, p % 16], kp[0, used[p // 16], :, p % 16])
