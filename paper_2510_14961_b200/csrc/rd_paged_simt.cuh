@@ -11,8 +11,8 @@
 //   reads being broadcasts), then DP / 32 output features for 8 rows.  K(t + 1) is requested behind Q K^T of
 //   tile t and V(t + 1) behind P V, so one buffer each suffices.
 //
-// A key no row of the tile sees is never multiplied: masked probabilities skip the V row, so what lies in
-// unwritten places of a page does not matter.
+// Keys no row of a tile sees are not read; a tile with a key that some row does not see goes key by key where V is not
+// finite (0 times an infinity would be a NaN), so what lies in unwritten places of a page does not matter.
 #pragma once
 #include "rd_paged.cuh"
 
@@ -73,8 +73,9 @@ __device__ __forceinline__ int pgs_row_position(const PgAttend& p, const PgPiece
 
 template <typename T, int DP> struct PgsFew {
     static constexpr int LD = DP + 16 / (int)sizeof(T);          // padded row: 16 bytes
-    static constexpr int STAGES = 3, KEYS = 8;
+    static constexpr int KEYS = 8;
     static constexpr int RUN = KEYS * LD * (int)sizeof(T);       // 8 rows of K or V
+    static constexpr int STAGES = 204800 / (16 * RUN) < 8 ? 204800 / (16 * RUN) : 8;      // as many as fit: bytes in flight are the stream's rate
     static constexpr int RING = 8 * STAGES * 2 * RUN;            // every warp's own
     static constexpr int QLD = DP + 4;
     static constexpr int Q_BYTES = PGS_FEW * QLD * 4;
@@ -91,6 +92,7 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_few_kernel(const __g
     uint8_t* ring = pgs_raw + C::Q_BYTES;
     __shared__ PgPlanSmem<PG_INLINE_REC> plan;
     __shared__ int flag;
+    __shared__ float4 Ps[8][C::KEYS];                              // per warp: probabilities of 8 keys for four rows
     pdl_enter();
     pg_plan_share<PGS_THREADS, PGS_KT>(p, M, plan);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, D = p.ge.D;
@@ -151,37 +153,81 @@ __global__ void __launch_bounds__(PGS_THREADS, 1) pg_attend_few_kernel(const __g
             float kk[DP / 4];
 #pragma unroll
             for (int c = 0; c < DP / 16; c++) pgs_f4(Kt + key_l * LD + c * 16 + quarter * 4, kk + c * 4);
+            float v[C::KEYS][E];
 #pragma unroll
-            for (int r = 0; r < M; r++) {
-                if (r >= rows) break;
-                float s = 0.f;
+            for (int j = 0; j < C::KEYS; j++)
 #pragma unroll
-                for (int c = 0; c < DP / 16; c++) {
-                    const float4 q = *reinterpret_cast<const float4*>(Qs + r * QLD + c * 16 + quarter * 4);
-                    s = fmaf(q.x, kk[c * 4], s); s = fmaf(q.y, kk[c * 4 + 1], s); s = fmaf(q.z, kk[c * 4 + 2], s); s = fmaf(q.w, kk[c * 4 + 3], s);
+                for (int e = 0; e < E; e++) v[j][e] = pg_to_f(Vt[j * LD + lane + 32 * e]);
+            const bool partial = pg_partial<PGS_KT>(key0 - warp * C::KEYS, pc.pmin, pc.pmax, p.window, p.sinks);
+            bool exact = false;                                    // an unseen key with a V that is not finite: 0 times it would be a NaN
+            if (partial) {
+                float probe = 0.f;
+#pragma unroll
+                for (int j = 0; j < C::KEYS; j++)
+#pragma unroll
+                    for (int e = 0; e < E; e++) probe = fmaf(v[j][e], 0.f, probe);
+                exact = __any_sync(0xffffffffu, probe != 0.f);
+            }
+            // four rows at a time: their reductions run next to each other, their probabilities go through shared memory once
+#pragma unroll
+            for (int r0 = 0; r0 < M; r0 += 4) {
+                if (r0 >= rows) break;
+                float s[4] = {0.f, 0.f, 0.f, 0.f}, mx[4];
+#pragma unroll
+                for (int c = 0; c < DP / 16; c++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        const float4 x = *reinterpret_cast<const float4*>(Qs + (r0 + q) * QLD + c * 16 + quarter * 4);
+                        s[q] = fmaf(x.x, kk[c * 4], s[q]); s[q] = fmaf(x.y, kk[c * 4 + 1], s[q]);
+                        s[q] = fmaf(x.z, kk[c * 4 + 2], s[q]); s[q] = fmaf(x.w, kk[c * 4 + 3], s[q]);
+                    }
+#pragma unroll
+                for (int w = 1; w < 4; w *= 2)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) s[q] += __shfl_xor_sync(0xffffffffu, s[q], w);
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    if (partial && !(pos[r0 + q] >= 0 && pg_sees(pos[r0 + q], key0 + key_l, p.window, p.sinks))) s[q] = -INFINITY;
+                    mx[q] = s[q];
                 }
-                s += __shfl_xor_sync(0xffffffffu, s, 1);
-                s += __shfl_xor_sync(0xffffffffu, s, 2);
-                const bool see = pos[r] >= 0 && pg_sees(pos[r], key0 + key_l, p.window, p.sinks);
-                float mx = see ? s : -INFINITY;
 #pragma unroll
-                for (int w = 4; w < 32; w *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                if (mx > m[r]) {
-                    const float f = exp2f(m[r] - mx);              // m = -inf: 0, nothing accumulated yet
-                    l[r] *= f;
+                for (int w = 4; w < 32; w *= 2)
 #pragma unroll
-                    for (int e = 0; e < E; e++) o[r][e] *= f;
-                    m[r] = mx;
+                    for (int q = 0; q < 4; q++) mx[q] = fmaxf(mx[q], __shfl_xor_sync(0xffffffffu, mx[q], w));
+                float4 pj;
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const float mn = fmaxf(m[r0 + q], mx[q]), u = mn == -INFINITY ? 0.f : mn, f = exp2f(m[r0 + q] - u);      // (0 while nothing was seen)
+                    m[r0 + q] = mn;
+                    const float x = exp2f(s[q] - u);
+                    l[r0 + q] = l[r0 + q] * f + (quarter == 0 ? x : 0.f);
+#pragma unroll
+                    for (int e = 0; e < E; e++) o[r0 + q][e] *= f;
+                    if (q == 0) pj.x = x; else if (q == 1) pj.y = x; else if (q == 2) pj.z = x; else pj.w = x;
                 }
-                const float pj = see ? exp2f(s - m[r]) : 0.f;
-                l[r] += quarter == 0 ? pj : 0.f;
-                const unsigned any = __ballot_sync(0xffffffffu, see);
+                if (quarter == 0) Ps[warp][key_l] = pj;
+                __syncwarp();
+#pragma unroll
                 for (int j = 0; j < C::KEYS; j++) {
-                    const float w = __shfl_sync(0xffffffffu, pj, j * 4);
-                    if (!(any >> (j * 4) & 1)) continue;           // V of an unseen key is not touched
+                    const float4 w = Ps[warp][j];
+                    if (!exact) {
 #pragma unroll
-                    for (int e = 0; e < E; e++) o[r][e] = fmaf(w, pg_to_f(Vt[j * LD + lane + 32 * e]), o[r][e]);
+                        for (int e = 0; e < E; e++) {
+                            o[r0][e] = fmaf(w.x, v[j][e], o[r0][e]); o[r0 + 1][e] = fmaf(w.y, v[j][e], o[r0 + 1][e]);
+                            o[r0 + 2][e] = fmaf(w.z, v[j][e], o[r0 + 2][e]); o[r0 + 3][e] = fmaf(w.w, v[j][e], o[r0 + 3][e]);
+                        }
+                    } else {
+                        const int jj = key0 + j;
+#pragma unroll
+                        for (int q = 0; q < 4; q++) {
+                            if (pos[r0 + q] < 0 || !pg_sees(pos[r0 + q], jj, p.window, p.sinks)) continue;
+                            const float wq = q == 0 ? w.x : q == 1 ? w.y : q == 2 ? w.z : w.w;
+#pragma unroll
+                            for (int e = 0; e < E; e++) o[r0 + q][e] = fmaf(wq, v[j][e], o[r0 + q][e]);
+                        }
+                    }
                 }
+                __syncwarp();
             }
             __syncwarp();                                          // the run is free for the next copy
         }
