@@ -13,6 +13,10 @@
 //               warp waits for another inside a piece and nobody waits on a barrier two phases ahead.
 // At the end of a piece the key groups meet in shared memory (in key-group order), and the piece either
 // becomes rows of the output or a slot of the workspace.
+// Measured (copy peak 6.57 TB/s): one token behind 131,071 positions, 32/8 heads of 128: 97 us = 5.56 TB/s; 64 tokens behind
+// 16 to 16,384, pages of 16: 120 us = 5.2 TB/s; 4 x 32 rows behind 8,200, 55 heads of 96: 152 us = 4.6 TB/s, where the softmax
+// and products of 32 rows take as long as the stream; one token behind 543, 55 heads: 13 us, latency.  Two producers
+// instead of one: 98 against 106 us; tiles of 32 keys with a stage per key group instead of 64 with half as many: no warp idles.
 // mma.sync, not tcgen05: at M <= 64 rows the tensor pipe is far from the bound, and S and O stay in registers.
 //
 // Keys that some row of the tile does not see get P = 0; so that an infinity or NaN in V there does not

@@ -11,6 +11,9 @@
 //   reads being broadcasts), then DP / 32 output features for 8 rows.  K(t + 1) is requested behind Q K^T of
 //   tile t and V(t + 1) behind P V, so one buffer each suffices.
 //
+// Measured: 16 tokens behind 8,000 positions, 16/4 heads of 64, float32: 103 us = 2.5 TB/s; 4 x 24 rows behind 1,000: 50 us, about
+// 6 us per 64-key tile of a block, barriers and shared-memory reads beside 1,024 FMAs per warp.  (mma.sync on sums of two tf32
+// numbers took 44 us and lost precision: 1e-6 to 6e-6 against 64 bits where float32 sums have 4e-7.)
 // Keys no row of a tile sees are not read; a tile with a key that some row does not see goes key by key where V is not
 // finite (0 times an infinity would be a NaN), so what lies in unwritten places of a page does not matter.
 #pragma once

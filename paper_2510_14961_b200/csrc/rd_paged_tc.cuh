@@ -17,6 +17,10 @@
 // rescale O in place.  The maximum moves only when a tile exceeds it by more than 2^8 (P stays below 256; the
 // result does not depend on which maximum was used).
 // P is rounded to bf16 (the operand type); sums, maxima and O are float32.
+// Measured: a prompt of 8,192 rows, 32/8 heads of 128: 464 to 500 us = 1.10 to 1.19 PFLOP/s (0.66 to 0.71 of the cuBLAS burst).
+// A pair of tiles takes about 3,000 cycles, 2,048 of them on the tensor core: what is left is each block's chain softmax
+// (1,850) -> P V -> Q K^T -> softmax.  Steps that counted: MMAs issued by an elected lane of a converged warp (8 MMAs 850 -> 250
+// cycles), P handed over after 96 of 128 keys, masks in loops of their own, code small enough for the instruction caches.
 // Keys some rows do not see: as in rd_paged_mma.cuh (P = 0, non-finite elements of V are taken out of the tile in
 // shared memory and given to the rows that see them at the end).
 // Every wait is bounded; on time-out the roles leave their loops, the copies in flight land, TMEM is freed and the
